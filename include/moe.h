@@ -347,6 +347,87 @@ int moe_pre_attention(const moe_linear_shape* qkv_proj, const float* hidden, con
                       float* hidden_out, void* x_norm, float* qkv, void* qkv_bf16, void* workspace, size_t workspace_bytes,
                       void* stream);
 
+/* ------------------------------------------------------------------ attention over a paged key-value cache
+ *
+ * What stands between moe_pre_attention and moe_post_attention when the key-value cache lives in device memory: the block
+ * tables and slot maps of a step, the norm and rotation of queries and keys with the write into the cache, and the attention
+ * of single tokens over it.  Arithmetic in float; dtype is the storage type of queries, attention output and cache.
+ *
+ * The cache of one layer is two arrays, K and V, each dtype[pool_pages][n_kv][page_tokens][head_dim].  Token t of a
+ * request is in page block_table[request][t / page_tokens] at place t % page_tokens; its SLOT is page * page_tokens + place.
+ * Entries of block tables, lengths and slots are device data that the host cannot check: kernels never follow a page or a slot
+ * outside the pool (a read takes page 0 instead, a write is left out) and set bit 0 of status[0].  status, where given, is
+ * device int32[4]; as with moe_expert_ffn kernels only OR bits into status[0], and the caller clears it.
+ *
+ * Supported: 1 <= n_kv, n_q a multiple of n_kv and at most MOE_MAX_HEADS, head_dim a multiple of 32 up to 256, page_tokens
+ * and max_pages at least 1, pool_pages * n_kv * page_tokens < 2^32, pool_pages * page_tokens and max_pages * page_tokens < 2^31.
+ */
+#define MOE_MAX_HEADS 1024
+#define MOE_MAX_REQUESTS 4096
+
+typedef struct moe_kv_shape {
+    int32_t n_q;         /* query heads */
+    int32_t n_kv;        /* key/value heads; query head h reads head h / (n_q / n_kv) */
+    int32_t head_dim;
+    int32_t page_tokens; /* tokens of a cache page */
+    int32_t max_pages;   /* entries of a request's row of the block table */
+    int32_t dtype;       /* MOE_DTYPE_* */
+    int64_t pool_pages;  /* pages of the cache */
+} moe_kv_shape;
+
+/* MOE_OK if the shape is one the library supports. */
+int moe_kv_validate(const moe_kv_shape* s);
+
+/* The tables of one step.  Request b has cached[b] tokens in the cache and brings fresh[b] more (0 is valid); the fresh
+ * tokens of all requests are rows 0, 1, .. in the order of the requests.  A request needs ceil((cached + fresh) /
+ * page_tokens) - ceil(cached / page_tokens) pages; these are taken from free_pages[free_head[0]], .. in the order of the
+ * requests and entered into its row of the block table behind the pages it has.  A request is REFUSED when one of its counts is
+ * negative (status bit 0), its rows would not end at or before T (bit 2), its pages would not fit its row of the table, or it
+ * needs pages and those of all requests up to it that pass these checks are more than are left (both bit 1): it gets no page, its length stays, and
+ * its rows have no slot.
+ *   cached, fresh: device int32[B]; free_pages: device int32[n_free]; free_head: device int32[1], how many of free_pages
+ *   are taken already; block_table: device int32[B][max_pages], entries of pages held are read, new ones written;
+ *   seq_len: device int32[B], cached + fresh (cached, at least 0, if refused); row_start: device int32[B + 1]; positions,
+ *   slots, request: device int32[T], the token's position, slot and request (0, -1, -1 for rows behind the last request's;
+ *   slot -1 for refused requests and pages outside the pool); free_head_out: device int32[1].
+ * B <= MOE_MAX_REQUESTS.  The outputs must not overlap the inputs: a caller keeps two sets of lengths and heads and takes
+ * them in turn. */
+int moe_kv_assign(const moe_kv_shape* s, int32_t B, int32_t T, const int32_t* cached, const int32_t* fresh,
+                  const int32_t* free_pages, int32_t n_free, const int32_t* free_head, int32_t* block_table,
+                  int32_t* seq_len, int32_t* row_start, int32_t* positions, int32_t* slots, int32_t* request,
+                  int32_t* free_head_out, int32_t* status, void* stream);
+
+/* Queries and keys of T rows: an RMS norm over each head with a learned scale, y = x / sqrt(mean(x^2) + eps) * gamma (left
+ * out where q_gamma / k_gamma is NULL), then the rotation of the first rot_dim elements by angle positions[t] *
+ * inv_freq[i]: (a, b) -> (a cos - b sin, b cos + a sin) on elements (i, i + rot_dim / 2), or with pairs != 0 on (2i, 2i + 1).
+ * Queries go to q, keys and values (only rounded) to the cache at slots[t]; a row with slot -1 leaves the cache alone.
+ *   qkv: device, float or bf16 (qkv_dtype) [T][row_elements], a row = n_q, n_kv and n_kv heads and whatever padding
+ *   follows, as moe_pre_attention's qkv; row_elements * element size a multiple of 16; q_gamma, k_gamma: device
+ *   float[head_dim]; inv_freq: device double[rot_dim / 2], radians per position; rot_dim a multiple of 8, 0 .. head_dim;
+ *   positions, slots: device int32[T]; q: device dtype[T][n_q][head_dim].  Two rows with one slot: either may be left.
+ * qkv, q and the cache 16-byte aligned. */
+int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t qkv_dtype, int64_t row_elements,
+                     const float* q_gamma, const float* k_gamma, float eps, const double* inv_freq, int32_t rot_dim,
+                     int32_t pairs, const int32_t* positions, const int32_t* slots, void* q, void* k_cache, void* v_cache,
+                     int32_t* status, void* stream);
+
+/* Attention of R rows, each one token: out[r][h] = sum_t p_t V[t], p = softmax over t of scale * q[r][h] . K[t], over tokens
+ * max(0, seq_len[r] - window) <= t < seq_len[r] (window 0: all) of the request whose block table row is table_row[r]
+ * (NULL: r).  No tokens, or table_row[r] = -1: out = 0, lse = -infinity.  A step of single tokens passes seq_len of
+ * moe_kv_assign; rows of prompts pass positions + 1 and request: the keys of a step's own tokens are in the cache by then.
+ *   q: device dtype[R][n_q][head_dim]; seq_len: device int32[R] (above max_pages * page_tokens: cut there, status bit 0);
+ *   block_table: device int32[table_rows][max_pages]; out: device dtype[R][n_q][head_dim]; lse: device float[R][n_q] or NULL,
+ *   natural logarithm of the sum of exponentials; workspace: device, 256-byte aligned, moe_attn_workspace_bytes.  Its first
+ *   MOE_ATTN_COUNTER_BYTES must be zero before its first use; every call leaves them zero, for any shape and R.
+ * A row's bits depend on how the rows of its call are split, and so on their lengths; equal calls give equal bits.
+ * q, out and the cache 16-byte aligned; R * ceil(max_pages * page_tokens / 16) < 2^31. */
+#define MOE_ATTN_COUNTER_BYTES 16384
+int moe_attn_workspace_bytes(const moe_kv_shape* s, int32_t R, size_t* bytes);
+int moe_attn_decode(const moe_kv_shape* s, int32_t R, const void* q, const int32_t* seq_len, const int32_t* table_row,
+                    const int32_t* block_table, int32_t table_rows, const void* k_cache, const void* v_cache, int32_t window,
+                    float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, int32_t* status,
+                    void* stream);
+
 /* ------------------------------------------------------------------ tuning knobs
  * Named integer options for experiments (kernel variants, tile order); unknown
  * names give MOE_ERR_INVALID_ARG.  The options are process-wide and read at launch

@@ -8,6 +8,7 @@ import of a symbol fails loudly; there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -88,6 +89,11 @@ _SIGNATURES = {
     "moe_post_attention_workspace_bytes": (ctypes.c_int, [_vp, _vp]),
     "moe_post_attention": (ctypes.c_int, [_vp] * 6 + [ctypes.c_float] + [_vp] * 4 + [_i64] + [_vp] * 4 + [_sz, _vp]),
     "moe_pre_attention": (ctypes.c_int, [_vp] * 4 + [ctypes.c_float, _vp, _vp, _i64] + [_vp] * 5 + [_sz, _vp]),
+    "moe_kv_validate": (ctypes.c_int, [_vp]),
+    "moe_kv_assign": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _i32] + [_vp] * 10),
+    "moe_qk_norm_rope": (ctypes.c_int, [_vp, _i32, _vp, _i32, _i64, _vp, _vp, ctypes.c_float, _vp, _i32, _i32] + [_vp] * 7),
+    "moe_attn_workspace_bytes": (ctypes.c_int, [_vp, _i32, _vp]),
+    "moe_attn_decode": (ctypes.c_int, [_vp, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i32, ctypes.c_float, _vp, _vp, _vp, _sz, _vp, _vp]),
     "moe_set_option": (ctypes.c_int, [ctypes.c_char_p, ctypes.c_int]),
     "moe_get_option": (ctypes.c_int, [ctypes.c_char_p, _vp]),
     "moe_profile_read": (ctypes.c_int, [_vp, _vp]),
@@ -659,3 +665,152 @@ def moe_pre_attention(qkv_proj: LinearShape, hidden, delta, norm_gamma, eps, qkv
                                     None if qkv16 is None else qkv16.data_ptr(), qkv.data_ptr(), 16, _stream(stream)),
            "moe_pre_attention")
     return hidden_out, x_norm, qkv, qkv16
+
+
+# ----------------------------------------------------------------------------- attention over a paged key-value cache
+
+class KvShape(ctypes.Structure):
+    """struct moe_kv_shape: heads, head size and page geometry of a paged key-value cache."""
+    _fields_ = [("n_q", _i32), ("n_kv", _i32), ("head_dim", _i32), ("page_tokens", _i32), ("max_pages", _i32), ("dtype", _i32),
+                ("pool_pages", _i64)]
+
+    @property
+    def torch_dtype(self):
+        return torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float32
+
+    @property
+    def cache_shape(self):
+        """Of K and of V: [pool_pages, n_kv, page_tokens, head_dim]."""
+        return (self.pool_pages, self.n_kv, self.page_tokens, self.head_dim)
+
+
+def make_kv_shape(n_q, n_kv, head_dim, page_tokens, max_pages, pool_pages, dtype) -> KvShape:
+    code = {"f32": 0, "bf16": 1, torch.float32: 0, torch.bfloat16: 1, 0: 0, 1: 1}[dtype]
+    return KvShape(int(n_q), int(n_kv), int(head_dim), int(page_tokens), int(max_pages), code, int(pool_pages))
+
+
+def kv_validate(kv: KvShape) -> int:
+    return _lib().moe_kv_validate(ctypes.byref(kv))
+
+
+def _on(stream):
+    """Memory that a call allocates belongs to the stream that the call goes to."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+class KvStep:
+    """The tables of one step, filled by moe_kv_assign: seq_len int32 [B], row_start int32 [B+1], positions, slots and
+    request int32 [T], free_head int32 [1].  A serving loop holds two and takes them in turn: seq_len and free_head of the
+    one are the next step's inputs."""
+
+    def __init__(self, kv: KvShape, B: int, T: int, device="cuda"):
+        self.kv, self.B, self.T = kv, int(B), int(T)
+        # each output 64-byte aligned
+        sizes = [("seq_len", self.B), ("row_start", self.B + 1), ("positions", self.T), ("slots", self.T), ("request", self.T), ("free_head", 1)]
+        starts, at = [], 0
+        for _, n in sizes:
+            starts.append(at)
+            at += (n + 15) // 16 * 16
+        self.buf = torch.zeros(at, dtype=torch.int32, device=device)
+        for (name, n), o in zip(sizes, starts):
+            setattr(self, name, self.buf[o:o + n])
+        base = self.buf.data_ptr()
+        self._ptrs = [base + 4 * o for o in starts]
+
+
+def moe_kv_assign(kv: KvShape, cached, fresh, free_pages, free_head, block_table, step: Optional[KvStep] = None, T: Optional[int] = None,
+                  status=None, stream=None) -> KvStep:
+    """Block tables and slot maps of a step with T rows (step.T, or T for a new KvStep)."""
+    B = cached.shape[0]
+    if step is None:
+        if T is None:
+            raise ValueError("moe_kv_assign: a step or the number of rows T is needed")
+        with _on(stream):
+            step = KvStep(kv, B, T, cached.device)
+    elif step.B != B:
+        raise ValueError(f"step: made for {step.B} requests, got {B}")
+    pc = _dev(cached, torch.int32, (B,), "cached")
+    pf = _dev(fresh, torch.int32, (B,), "fresh")
+    pp = _dev(free_pages, torch.int32, (free_pages.shape[0],), "free_pages")
+    ph = _dev(free_head, torch.int32, (1,), "free_head")
+    pt = _dev(block_table, torch.int32, (B, kv.max_pages), "block_table")
+    ps = _dev(status, torch.int32, (4,), "status")
+    o = step._ptrs
+    _check(_lib().moe_kv_assign(ctypes.byref(kv), B, step.T, pc, pf, pp, free_pages.shape[0], ph, pt, o[0], o[1], o[2], o[3], o[4], o[5], ps,
+                                _stream(stream)), "moe_kv_assign")
+    return step
+
+
+def moe_qk_norm_rope(kv: KvShape, qkv, inv_freq, positions, slots, k_cache, v_cache, q_gamma=None, k_gamma=None, eps: float = 1e-5,
+                     pairs: bool = False, q: Optional[torch.Tensor] = None, status=None, stream=None) -> torch.Tensor:
+    """qkv float32 or bf16 [T, n >= (n_q + 2 n_kv) * head_dim]; inv_freq float64 [rot_dim / 2].  -> q dtype [T, n_q, head_dim];
+    keys and values go to the cache."""
+    T, n = qkv.shape
+    dt = kv.torch_dtype
+    if qkv.dtype is not torch.bfloat16 and qkv.dtype is not torch.float32:
+        raise TypeError(f"qkv: expected torch.float32 or torch.bfloat16, got {qkv.dtype}")
+    px = _dev(qkv, qkv.dtype, None, "qkv")
+    pi = _dev(inv_freq, torch.float64, (inv_freq.shape[0],), "inv_freq")
+    pp = _dev(positions, torch.int32, (T,), "positions")
+    ps = _dev(slots, torch.int32, (T,), "slots")
+    pk = _dev(k_cache, dt, kv.cache_shape, "k_cache")
+    pv = _dev(v_cache, dt, kv.cache_shape, "v_cache")
+    gq = _dev(q_gamma, torch.float32, (kv.head_dim,), "q_gamma")
+    gk = _dev(k_gamma, torch.float32, (kv.head_dim,), "k_gamma")
+    pst = _dev(status, torch.int32, (4,), "status")
+    if q is None:
+        with _on(stream):
+            q = torch.empty((T, kv.n_q, kv.head_dim), dtype=dt, device=qkv.device)
+    pq = _dev(q, dt, (T, kv.n_q, kv.head_dim), "q")
+    _check(_lib().moe_qk_norm_rope(ctypes.byref(kv), T, px, DTYPE_BF16 if qkv.dtype is torch.bfloat16 else DTYPE_F32, n, gq, gk, eps, pi,
+                                   2 * inv_freq.shape[0], 1 if pairs else 0, pp, ps, pq, pk, pv, pst, _stream(stream)), "moe_qk_norm_rope")
+    return q
+
+
+@functools.lru_cache(maxsize=256)
+def _attn_workspace_bytes(R, *fields):
+    v = _sz(0)
+    _check(_lib().moe_attn_workspace_bytes(ctypes.byref(KvShape(*fields)), R, ctypes.byref(v)), "moe_attn_workspace_bytes")
+    return int(v.value)
+
+
+def attn_workspace_bytes(kv: KvShape, R: int) -> int:
+    return _attn_workspace_bytes(int(R), kv.n_q, kv.n_kv, kv.head_dim, kv.page_tokens, kv.max_pages, kv.dtype, kv.pool_pages)
+
+
+class AttnWorkspace:
+    """Device scratch of moe_attn_decode for up to R rows, its counters zeroed."""
+
+    def __init__(self, kv: KvShape, R: int, device="cuda"):
+        self.buf = torch.zeros(attn_workspace_bytes(kv, R), dtype=torch.uint8, device=device)
+        if self.buf.data_ptr() % 256:
+            raise RuntimeError("allocator returned an unaligned workspace")
+
+
+def moe_attn_decode(kv: KvShape, q, seq_len, block_table, k_cache, v_cache, scale: Optional[float] = None, window: int = 0, table_row=None,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                    workspace: Optional[AttnWorkspace] = None, status=None, stream=None):
+    """-> (out dtype [R, n_q, head_dim], lse float32 [R, n_q] or None); scale None: 1 / sqrt(head_dim)."""
+    R = q.shape[0]
+    dt = kv.torch_dtype
+    shape = (R, kv.n_q, kv.head_dim)
+    pq = _dev(q, dt, shape, "q")
+    pl = _dev(seq_len, torch.int32, (R,), "seq_len")
+    pr = _dev(table_row, torch.int32, (R,), "table_row")
+    pt = _dev(block_table, torch.int32, (block_table.shape[0], kv.max_pages), "block_table")
+    pk = _dev(k_cache, dt, kv.cache_shape, "k_cache")
+    pv = _dev(v_cache, dt, kv.cache_shape, "v_cache")
+    ps = _dev(status, torch.int32, (4,), "status")
+    if out is None or workspace is None or (want_lse and lse is None):
+        with _on(stream):
+            out = torch.empty(shape, dtype=dt, device=q.device) if out is None else out
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if want_lse and lse is None else lse
+            workspace = AttnWorkspace(kv, R, q.device) if workspace is None else workspace
+    po = _dev(out, dt, shape, "out")
+    ple = _dev(lse, torch.float32, shape[:2], "lse")
+    _check(_lib().moe_attn_decode(ctypes.byref(kv), R, pq, pl, pr, pt, block_table.shape[0], pk, pv, int(window),
+                                  kv.head_dim ** -0.5 if scale is None else scale, po, ple, workspace.buf.data_ptr(), workspace.buf.numel(), ps,
+                                  _stream(stream)), "moe_attn_decode")
+    return out, lse

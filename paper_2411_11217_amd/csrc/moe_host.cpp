@@ -39,6 +39,18 @@ Geom geometry(const moe_shape& s) {
     return g;
 }
 
+int validate_kv(const moe_kv_shape* s) {
+    if (!s) return MOE_ERR_INVALID_ARG;
+    if (s->dtype != MOE_DTYPE_F32 && s->dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED_DTYPE;
+    if (s->n_kv < 1 || s->n_q < s->n_kv || s->n_q > MOE_MAX_HEADS || s->n_q % s->n_kv != 0) return MOE_ERR_INVALID_ARG;
+    if (s->head_dim < 32 || s->head_dim > 256 || s->head_dim % 32 != 0) return MOE_ERR_INVALID_ARG;
+    if (s->page_tokens < 1 || s->max_pages < 1 || s->pool_pages < 1 || s->pool_pages > INT32_MAX) return MOE_ERR_INVALID_ARG;
+    if ((int64_t)s->max_pages * s->page_tokens > INT32_MAX || s->pool_pages * s->page_tokens > INT32_MAX ||
+        s->pool_pages * s->page_tokens * s->n_kv > (int64_t)UINT32_MAX)
+        return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
 // ---- packer -------------------------------------------------------------------
 // Byte offset inside a page tile of the 16-byte chunk c of row n (the page format of moe.h).
 // bf16: two half-tiles of 128 rows x 64 bytes, chunk c & 3 of half c >> 2 at position
@@ -150,6 +162,8 @@ const char* moe_status_string(int status) {
         default: return "unknown status";
     }
 }
+
+int moe_kv_validate(const moe_kv_shape* s) { return moe::validate_kv(s); }
 
 int moe_validate_shape(const moe_shape* s) { return validate_shape(s); }
 

@@ -48,6 +48,9 @@ inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 int validate_linear(const moe_linear_shape* s);
 int64_t linear_pages(const moe_linear_shape& s);
 
+// Attention over a paged cache: MOE_OK or an error.
+int validate_kv(const moe_kv_shape* s);
+
 // Where the dense linear map takes the kernel for few rows (csrc/moe_ffn_rows_bf16.hip): as long as blocks of 64 columns and 128
 // rows, or with more than 128 rows of 128 columns and 64 rows, make one round on the 256 compute units (which blocks it has
 // then is linear_rows_block's choice), and with a short k and few rows.

@@ -1,0 +1,579 @@
+"""Attention over a paged cache on the GPU, through the C ABI, against oracle/attention.py: tables and slots bit by
+bit, norm and rotation and the attention within bounds that the oracle derives from the arithmetic."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_11217_amd as M
+from oracle import attention
+from paper_2411_11217_amd import binding as B
+from util import say
+
+pytestmark = pytest.mark.gpu
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}       # a rounding is off by at most half a step
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def i32(a):
+    return torch.as_tensor(np.ascontiguousarray(a), dtype=torch.int32).cuda()
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def new_status():
+    return torch.zeros(4, dtype=torch.int32, device="cuda")
+
+
+def within(got, ref, bound, dtype, what):
+    """bound: what the arithmetic before the last rounding may be off by."""
+    got = np.asarray(got, np.float64)
+    assert got.shape == ref.shape and np.isfinite(got).all(), what
+    room = bound + HALF_STEP[dtype] * (np.abs(ref) + bound) + 1e-38
+    err = np.abs(got - ref)
+    worst = float((err / room).max()) if err.size else 0.0
+    say(f"    {what}: max|err|={float(err.max()) if err.size else 0.0:.3e}, {worst:.3f} of what is allowed")
+    assert worst <= 1.0, what
+
+
+# ---------------------------------------------------------------------------- tables and slots
+
+def tables(B_, page, width, pool, seed, cached=None):
+    """Block table with the cached tokens' pages at shuffled places, and the other pages."""
+    g = np.random.default_rng(seed)
+    held = -(-np.maximum(cached, 0).astype(np.int64) // page)
+    order = g.permutation(pool).astype(np.int32)
+    table = np.full((B_, width), -1, np.int32)
+    at = 0
+    for b in range(B_):
+        n = min(int(held[b]), width)
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table, order[at:]
+
+
+def assign_and_compare(page, width, pool, T, cached, fresh, free, head, table):
+    kv = M.make_kv_shape(1, 1, 32, page, width, pool, "bf16")
+    ref = attention.assign(page, width, pool, T, cached, fresh, free, head, table)
+    status, dev = new_status(), i32(table)
+    step = M.moe_kv_assign(kv, i32(cached), i32(fresh), i32(free), i32([head]), dev, T=T, status=status)
+    torch.cuda.synchronize()
+    for name in ("seq_len", "row_start", "positions", "slots", "request", "free_head"):
+        assert np.array_equal(getattr(step, name).cpu().numpy(), ref[name]), name
+    assert np.array_equal(dev.cpu().numpy(), ref["block_table"])
+    assert status.tolist() == [ref["status"], 0, 0, 0]
+    return ref
+
+
+@pytest.mark.parametrize("B_,page,most,new,pad", [
+    (1, 16, 0, 1, 0), (1, 16, 16, 1, 0), (1, 16, 15, 1, 3), (1, 1, 5, 3, 0), (1, 7, 100, 3000, 0), (2, 16, 0, 0, 0), (5, 16, 40, 0, 4), (36, 16, 700, 1, 0),
+    (255, 5, 90, 4, 1), (256, 64, 5000, 1, 0), (257, 3, 50, 9, 77), (1000, 16, 3, 40, 0), (4096, 16, 900, 3, 5), (4095, 1, 2, 2, 0), (600, 256, 100000, 700, 0),
+])
+def test_assign(B_, page, most, new, pad):
+    g = np.random.default_rng(B_ * 31 + page)
+    cached, fresh = g.integers(0, most + 1, B_), g.integers(0 if B_ > 1 and new else new, new + 1, B_)
+    width = int((cached + fresh).max()) // page + 2
+    pool = int((-(-(cached + fresh) // page)).sum()) + 9
+    table, free = tables(B_, page, width, pool, 1, cached)
+    ref = assign_and_compare(page, width, pool, int(fresh.sum()) + pad, cached, fresh, free, 0, table)
+    assert ref["status"] == 0
+
+
+@pytest.mark.parametrize("what", ["pages", "pages_later", "rows", "width", "negative", "head", "no_free", "bad_page", "bad_free", "huge", "everything"])
+@pytest.mark.parametrize("B_", [7, 300])
+def test_assign_refuses_requests(what, B_):
+    g = np.random.default_rng(B_)
+    page, width, pool = 4, 12, 5000
+    cached, fresh = g.integers(0, 20, B_), g.integers(0, 9, B_)
+    cached[0], fresh[0], fresh[-1] = 5, 6, 3
+    table, free = tables(B_, page, width, pool, 2, cached)
+    T, head = int(fresh.sum()) + 2, 3
+    if what in ("pages", "pages_later", "everything"):
+        free = free[:head + (1 if what == "pages" else B_ // 2)]
+    if what in ("rows", "everything"):
+        T = int(fresh.sum()) * 2 // 3
+    if what in ("width", "everything"):
+        fresh[B_ // 2] = 60
+    if what in ("negative", "everything"):
+        cached[2], fresh[3], fresh[4] = -5, -1, -2 ** 31
+    if what == "head":
+        head = len(free) + 1
+    if what == "no_free":
+        free, head = free[:0], 0
+    if what == "bad_page":
+        table[0, 1], table[1, :] = -7, pool
+        cached[0] = 6
+    if what == "bad_free":
+        free[3:8] = [-1, pool, 2 ** 31 - 1, -2 ** 31, 5]
+    if what == "huge":
+        cached[1], fresh[2], cached[5], fresh[5] = 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1
+        T = 900
+    ref = assign_and_compare(page, width, pool, T, cached, fresh, free, head, table)
+    assert ref["status"] != 0
+
+
+def test_assign_takes_steps_in_turn():
+    # two KvSteps: lengths and the head of the one are inputs of the next; pages fill up, and the last steps refuse
+    B_, page, width, pool = 33, 4, 20, 200
+    kv = M.make_kv_shape(1, 1, 32, page, width, pool, "bf16")
+    g = np.random.default_rng(5)
+    free = g.permutation(pool).astype(np.int32)
+    table = np.full((B_, width), -1, np.int32)
+    dev, steps = i32(table), [M.KvStep(kv, B_, 120), M.KvStep(kv, B_, 120)]
+    seq, head, first = np.zeros(B_, np.int64), 0, True
+    for n in range(12):
+        fresh = g.integers(0, 6, B_)
+        ref = attention.assign(page, width, pool, 120, seq, fresh, free, head, table)
+        prev, step = steps[(n + 1) % 2], steps[n % 2]
+        M.moe_kv_assign(kv, i32(seq) if first else prev.seq_len, i32(fresh), i32(free), i32([0]) if first else prev.free_head, dev, step=step)
+        torch.cuda.synchronize()
+        for name in ("seq_len", "row_start", "positions", "slots", "request", "free_head"):
+            assert np.array_equal(getattr(step, name).cpu().numpy(), ref[name]), (n, name)
+        table, seq, head, first = ref["block_table"], ref["seq_len"], int(ref["free_head"][0]), False
+        assert np.array_equal(dev.cpu().numpy(), table)
+    assert head > 150
+
+
+# ---------------------------------------------------------------------------- norm, rotation, cache
+
+def rope_case(T, n_q, n_kv, D, P, x_dtype, dtype, rot, pairs, norm, seed, far=40000, extra=0, std=1.5):
+    g = torch.Generator().manual_seed(seed)
+    width = (n_q + 2 * n_kv) * D + extra
+    pages = -(-T // P) + 2
+    kv = M.make_kv_shape(n_q, n_kv, D, P, 1, pages, dtype)
+    x = (torch.randn((T, width), generator=g) * std).to(DT[x_dtype])
+    freq = torch.tensor([10000.0 ** (-2.0 * i / max(rot, 1)) for i in range(rot // 2)], dtype=torch.float64)
+    pos = torch.randint(0, far, (T,), generator=g, dtype=torch.int32)
+    slots = torch.randperm(pages * P, generator=g)[:T].to(torch.int32)
+    gammas = [1.0 + 0.2 * torch.randn((D,), generator=g) if norm else None for _ in range(2)]
+    caches = [torch.randn(kv.cache_shape, generator=g).to(DT[dtype]) for _ in range(2)]
+    return kv, x, freq, pos, slots, gammas, caches
+
+
+def rope_and_compare(kv, x, freq, pos, slots, gammas, caches, dtype, pairs, want_status=0, eps=1e-5, **kw):
+    n_q, n_kv, D, P, T = kv.n_q, kv.n_kv, kv.head_dim, kv.page_tokens, x.shape[0]
+    status = new_status()
+    dev = [c.cuda() for c in caches]
+    q = M.moe_qk_norm_rope(kv, x.cuda(), freq.cuda(), pos.cuda(), slots.cuda(), *dev, *[None if w is None else w.cuda() for w in gammas], eps=eps, pairs=pairs, status=status, **kw)
+    torch.cuda.synchronize()
+    assert status.tolist() == [want_status, 0, 0, 0]
+    heads = f64(x)[:, :(n_q + 2 * n_kv) * D].reshape(T, -1, D)
+    want_q, bound_q = attention.qk_norm_rope(heads[:, :n_q], None if gammas[0] is None else f64(gammas[0]), eps, freq.numpy(), pos.numpy(), pairs)
+    want_k, bound_k = attention.qk_norm_rope(heads[:, n_q:n_q + n_kv], None if gammas[1] is None else f64(gammas[1]), eps, freq.numpy(), pos.numpy(), pairs)
+    within(f64(q), want_q, bound_q, dtype, "q")
+    rows = np.nonzero((slots.numpy() >= 0) & (slots.numpy() < kv.pool_pages * P))[0]
+    page, place = slots.numpy()[rows] // P, slots.numpy()[rows] % P
+    k_dev, v_dev = dev[0].cpu(), dev[1].cpu()
+    within(f64(k_dev[page, :, place]), want_k[rows], bound_k[rows], dtype, "k")
+    want_v = caches[1].clone()
+    want_v[page, :, place] = x[:, (n_q + n_kv) * D:(n_q + 2 * n_kv) * D].reshape(T, n_kv, D)[rows].to(DT[dtype])
+    assert torch.equal(v_dev, want_v)
+    k_dev[page, :, place] = caches[0][page, :, place]
+    assert torch.equal(k_dev, caches[0])                   # nothing but the slots was written
+    return q
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("x_dtype,dtype", [("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")])
+def test_norm_rope_sizes(D, x_dtype, dtype):
+    for pairs in (False, True):
+        for rot in sorted({0, 8, D // 2, D}):
+            T, n_q, n_kv, P = 5 + rot % 7, 6, 2, 7
+            case = rope_case(T, n_q, n_kv, D, P, x_dtype, dtype, rot, pairs, rot != 8, D + rot)
+            rope_and_compare(*case, dtype, pairs)
+
+
+@pytest.mark.parametrize("T,n_q,n_kv", [(1, 1, 1), (1, 32, 8), (2, 20, 20), (3, 7, 1), (63, 48, 8), (300, 5, 5), (1500, 3, 1), (700, 32, 8)])
+@pytest.mark.parametrize("pairs", [False, True])
+def test_norm_rope_rows_and_heads(T, n_q, n_kv, pairs):
+    rope_and_compare(*rope_case(T, n_q, n_kv, 128, 16, "f32", "bf16", 128, pairs, True, T + n_q, far=1 << 24, extra=128), "bf16", pairs)
+
+
+def test_norm_rope_leaves_out_rows_without_slots():
+    case = list(rope_case(40, 4, 2, 64, 16, "f32", "bf16", 64, False, True, 3))
+    case[4][5] = case[4][39] = -1
+    rope_and_compare(*case, "bf16", False)
+    case[4][7], case[4][9], case[4][11] = case[0].pool_pages * 16, -2, -2 ** 31      # outside the pool: left out as well, and reported
+    rope_and_compare(*case, "bf16", False, want_status=1)
+    case[4][:] = -1
+    rope_and_compare(*case, "bf16", False)
+
+
+def test_norm_rope_one_norm_alone_and_large_values():
+    case = list(rope_case(33, 4, 2, 96, 5, "f32", "f32", 96, True, True, 4, std=300.0))
+    case[5] = [None, case[5][1]]
+    rope_and_compare(*case, "f32", True)
+    case[5] = [case[5][1], None]
+    rope_and_compare(*case, "f32", True)
+    case[1][3] = 0.0                                       # a row of zeros: eps alone under the root
+    rope_and_compare(*case, "f32", True)
+    rope_and_compare(*rope_case(9, 2, 1, 64, 4, "f32", "bf16", 64, False, True, 6, std=1e-12), "bf16", False)
+
+
+def test_norm_rope_keeps_bad_values_in_their_head():
+    kv, x, freq, pos, slots, gammas, caches = rope_case(6, 4, 2, 64, 4, "f32", "bf16", 64, False, True, 8)
+    clean = rope_and_compare(kv, x, freq, pos, slots, gammas, caches, "bf16", False)
+    x[2, 64 + 3], x[4, 2 * 64 + 9] = float("nan"), float("inf")
+    q = M.moe_qk_norm_rope(kv, x.cuda(), freq.cuda(), pos.cuda(), slots.cuda(), *[c.cuda() for c in caches], *[w.cuda() for w in gammas])
+    torch.cuda.synchronize()
+    other = torch.ones(6, 4, dtype=torch.bool)
+    other[2, 1] = other[4, 2] = False
+    assert torch.equal(q.cpu()[other], clean.cpu()[other]) and q[2, 1].isnan().all() and q[4, 2].isnan().any()
+
+
+# ---------------------------------------------------------------------------- attention
+
+class Cache:
+    """A paged cache with the given requests' keys and values at shuffled pages, and everything else NaN."""
+
+    def __init__(self, lens, n_kv, D, P, dtype, seed, pool=None, std=1.0, width=None):
+        g = torch.Generator().manual_seed(seed)
+        self.lens, self.P = list(lens), P
+        held = [-(-n // P) for n in lens]
+        pool = sum(held) + 3 if pool is None else pool
+        order = torch.randperm(pool, generator=g)
+        self.table = torch.full((len(lens), max(held + [1]) if width is None else width), -1, dtype=torch.int32)
+        self.k = torch.full((pool, n_kv, P, D), float("nan"), dtype=DT[dtype])
+        self.v = torch.full((pool, n_kv, P, D), float("nan"), dtype=DT[dtype])
+        self.keys, self.values, at = [], [], 0
+        for b, n in enumerate(lens):
+            k, v = (torch.randn((n, n_kv, D), generator=g) * std).to(DT[dtype]), torch.randn((n, n_kv, D), generator=g).to(DT[dtype])
+            pages = order[at:at + held[b]]
+            at += held[b]
+            self.table[b, :held[b]] = pages.to(torch.int32)
+            t = torch.arange(n)
+            self.k[pages[t // P], :, t % P], self.v[pages[t // P], :, t % P] = k, v
+            self.keys.append(k)
+            self.values.append(v)
+
+
+def attend_and_compare(c, kv, q, seq_len, dtype, window=0, scale=None, table_row=None, rows=None, want_status=0, workspace=None, dev=None, what=""):
+    """rows: the rows to check against the oracle (all)."""
+    R, G, D = q.shape[0], kv.n_q // kv.n_kv, kv.head_dim
+    dev = dev or (c.table.cuda(), c.k.cuda(), c.v.cuda())
+    status = new_status()
+    out, lse = M.moe_attn_decode(kv, q.cuda(), i32(seq_len), *dev, scale=scale, window=window, table_row=None if table_row is None else i32(table_row), want_lse=True,
+                                 workspace=workspace, status=status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [want_status, 0, 0, 0]
+    used = D ** -0.5 if scale is None else scale
+    got, got_lse = f64(out), f64(lse)
+    rows = range(R) if rows is None else rows
+    refs, bounds = np.zeros((len(rows), kv.n_q, D)), np.zeros((len(rows), kv.n_q, D))
+    for i, r in enumerate(rows):
+        b, n = (r if table_row is None else table_row[r]), seq_len[r]
+        n = 0 if b < 0 or b >= len(c.lens) else max(n, 0)
+        first = max(0, n - window) if window else 0
+        for h in range(kv.n_kv):
+            heads = slice(h * G, (h + 1) * G)
+            if n == 0:
+                assert (got_lse[r, heads] == -np.inf).all() and (got[r, heads] == 0).all()
+                continue
+            refs[i, heads], ref_lse, bounds[i, heads], lse_bound = attention.attend(f64(q[r, heads]), f64(c.keys[b][first:n, h]), f64(c.values[b][first:n, h]), used, dtype == "bf16")
+            assert (np.abs(got_lse[r, heads] - ref_lse) <= lse_bound + 2.0 ** -24 * np.abs(ref_lse)).all(), (r, h, got_lse[r, heads], ref_lse)
+    within(got[list(rows)], refs, bounds, dtype, what or f"R={R}")
+    return out, lse
+
+
+def queries(R, kv, dtype, seed, std=2.0):
+    return (torch.randn((R, kv.n_q, kv.head_dim), generator=torch.Generator().manual_seed(seed)) * std).to(DT[dtype])
+
+
+EDGE_LENS = [0, 1, 2, 3, 4, 5, 8, 15, 16, 17, 31, 32, 33, 47, 48, 63, 64, 65, 100, 127, 128, 129, 0, 255, 256, 257, 300]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_attention_head_sizes(D, dtype):
+    for n_q, n_kv, P in ((4, 2, 16), (3, 3, 7)):
+        c = Cache(EDGE_LENS, n_kv, D, P, dtype, D)
+        kv = M.make_kv_shape(n_q, n_kv, D, P, c.table.shape[1], c.k.shape[0], dtype)
+        attend_and_compare(c, kv, queries(len(EDGE_LENS), kv, dtype, D + 1), EDGE_LENS, dtype, what=f"D={D} P={P}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (2, 1), (5, 1), (15, 1), (16, 1), (17, 1), (24, 1), (33, 1), (64, 2), (40, 20), (128, 8), (1024, 64)])
+def test_attention_groups_of_heads(n_q, n_kv, dtype):
+    lens = [0, 1, 33, 70, 200] if n_q < 1000 else [1, 40]
+    c = Cache(lens, n_kv, 64, 16, dtype, n_q)
+    kv = M.make_kv_shape(n_q, n_kv, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+    attend_and_compare(c, kv, queries(len(lens), kv, dtype, n_q), lens, dtype, what=f"heads {n_q}/{n_kv}")
+
+
+@pytest.mark.parametrize("P", [1, 2, 3, 5, 8, 16, 31, 32, 33, 64, 100, 256, 1000])
+@pytest.mark.parametrize("window", [0, 1, 16, 40, 250])
+def test_attention_pages_and_windows(P, window):
+    for dtype in ("bf16", "f32"):
+        c = Cache(EDGE_LENS, 2, 64, P, dtype, P)
+        kv = M.make_kv_shape(6, 2, 64, P, c.table.shape[1], c.k.shape[0], dtype)
+        attend_and_compare(c, kv, queries(len(EDGE_LENS), kv, dtype, P + 1), EDGE_LENS, dtype, window=window, what=f"P={P} window={window} {dtype}")
+
+
+@pytest.mark.parametrize("dtype,lens,n_q,n_kv,D,P,window", [
+    ("bf16", [9000], 8, 2, 128, 16, 0),                        # one request over many blocks
+    ("f32", [5000], 4, 2, 128, 16, 0),
+    ("bf16", [20011, 1, 0, 777], 6, 1, 128, 32, 0),
+    ("bf16", [1] * 700, 2, 1, 64, 16, 0),                      # many rows of one token
+    ("bf16", [0] * 300 + [5] * 300, 2, 2, 64, 16, 0),
+    ("bf16", [(i * 37) % 400 for i in range(300)], 4, 2, 64, 16, 0),
+    ("f32", [(i * 53) % 300 for i in range(270)], 4, 2, 64, 7, 0),
+    ("bf16", [4000, 30, 30, 30, 4000, 0, 0, 2000], 20, 4, 96, 5, 0),
+    ("bf16", [12000] * 3, 4, 2, 128, 64, 3000),
+    ("bf16", [6000, 6001], 2, 2, 256, 16, 0),
+    ("f32", [3000, 10], 34, 2, 256, 16, 0),
+    ("bf16", [7000], 48, 1, 64, 16, 0),
+])
+def test_attention_splits_and_joins(dtype, lens, n_q, n_kv, D, P, window):
+    c = Cache(lens, n_kv, D, P, dtype, 17)
+    kv = M.make_kv_shape(n_q, n_kv, D, P, c.table.shape[1], c.k.shape[0], dtype)
+    q = queries(len(lens), kv, dtype, 3)
+    dev = (c.table.cuda(), c.k.cuda(), c.v.cuda())
+    rows = range(len(lens)) if len(lens) < 20 else range(0, len(lens), 7)
+    out, lse = attend_and_compare(c, kv, q, lens, dtype, window=window, rows=rows, dev=dev)
+    again, lse2 = M.moe_attn_decode(kv, q.cuda(), i32(lens), *dev, window=window, want_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_attention_more_rows_than_are_scanned_at_once():
+    # 30000 rows, most of them one token of one request seen at different lengths, through table_row
+    lens = [50, 300, 7]
+    c = Cache(lens, 1, 64, 16, "bf16", 2)
+    kv = M.make_kv_shape(2, 1, 64, 16, c.table.shape[1], c.k.shape[0], "bf16")
+    R = 30000
+    rows = [i % 3 for i in range(R)]
+    seq = [1 + (i * 7) % lens[b] for i, b in enumerate(rows)]
+    attend_and_compare(c, kv, queries(R, kv, "bf16", 1), seq, "bf16", table_row=rows, rows=list(range(0, R, 501)) + [R - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_prompt_rows(dtype):
+    # every token of two prompts a row, padding rows (-1) between and behind
+    lens = [70, 45]
+    c = Cache(lens, 2, 128, 16, dtype, 5)
+    kv = M.make_kv_shape(8, 2, 128, 16, c.table.shape[1], c.k.shape[0], dtype)
+    rows = [0] * 70 + [-1, -1] + [1] * 45 + [-1] * 3
+    seq = list(range(1, 71)) + [9, 0] + list(range(1, 46)) + [1, 2, 3]
+    attend_and_compare(c, kv, queries(len(rows), kv, dtype, 1), seq, dtype, table_row=rows)
+    attend_and_compare(c, kv, queries(len(rows), kv, dtype, 2), seq, dtype, table_row=rows, window=13)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_extreme_scores(dtype):
+    c = Cache([1, 40, 513], 2, 64, 16, dtype, 9, std=30.0)
+    kv = M.make_kv_shape(4, 2, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+    q = queries(3, kv, dtype, 1, std=30.0)
+    attend_and_compare(c, kv, q, c.lens, dtype, scale=1.0)               # scores of thousands
+    attend_and_compare(c, kv, q, c.lens, dtype, scale=-0.5)
+    attend_and_compare(c, kv, q, c.lens, dtype, scale=0.0)
+    attend_and_compare(c, kv, q * 0, c.lens, dtype)
+    tiny = (q.float() * 1e-30).to(DT[dtype])
+    attend_and_compare(c, kv, tiny, c.lens, dtype)
+
+
+def test_attention_bad_values_stay_in_their_row_and_head():
+    lens = [40, 300, 17, 90]
+    for dtype in ("bf16", "f32"):
+        c = Cache(lens, 2, 64, 16, dtype, 4)
+        kv = M.make_kv_shape(4, 2, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+        q = queries(4, kv, dtype, 7)
+        clean, _ = attend_and_compare(c, kv, q, lens, dtype)
+        c.k[c.table[1, 3], 1, 2, 5] = float("nan")                     # row 1, key/value head 1
+        c.v[c.table[2, 0], 0, 3, 9] = float("inf")                     # row 2, key/value head 0, element 9
+        q[3, 0, 1] = float("nan")                                      # row 3, head 0
+        out, _ = M.moe_attn_decode(kv, q.cuda(), i32(lens), c.table.cuda(), c.k.cuda(), c.v.cuda())
+        torch.cuda.synchronize()
+        same = torch.ones((4, 4, 64), dtype=torch.bool)
+        same[1, 2:] = same[3, 0] = False
+        same[2, :2, 9] = False
+        assert torch.equal(out.cpu()[same], clean.cpu()[same])
+        assert out[1, 2:].isnan().all() and out[3, 0].isnan().all() and not out[2, :2, 9].isfinite().any()
+
+
+def test_attention_pages_outside_the_pool():
+    # their tokens are read from page 0, which is in the pool; the status says so, and other rows are as they were
+    lens = [100, 64, 33]
+    c = Cache(lens, 2, 64, 16, "bf16", 6)
+    kv = M.make_kv_shape(4, 2, 64, 16, c.table.shape[1], c.k.shape[0], "bf16")
+    q = queries(3, kv, "bf16", 7)
+    clean, _ = attend_and_compare(c, kv, q, lens, "bf16")
+    for bad in (-1, c.k.shape[0], 2 ** 31 - 1, -2 ** 31):
+        table, status = c.table.clone(), new_status()
+        table[0, 2] = bad
+        out, _ = M.moe_attn_decode(kv, q.cuda(), i32(lens), table.cuda(), c.k.cuda(), c.v.cuda(), status=status)
+        torch.cuda.synchronize()
+        assert status.tolist() == [1, 0, 0, 0] and torch.equal(out[1:], clean[1:])
+    # entries behind a row's length, or before its window, are never followed
+    table, status = c.table.clone(), new_status()
+    table[1, 4:], table[2, 3:], table[1, 0] = 12345678, -9, -1
+    out, _ = M.moe_attn_decode(kv, q.cuda(), i32(lens), table.cuda(), c.k.cuda(), c.v.cuda(), window=33, status=status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [0, 0, 0, 0] and torch.equal(out[2], clean[2])
+
+
+def test_attention_lengths_and_rows_that_do_not_fit():
+    lens = [48, 20]
+    c = Cache(lens, 1, 64, 16, "bf16", 6)                  # rows of three pages
+    kv = M.make_kv_shape(2, 1, 64, 16, 3, c.k.shape[0], "bf16")
+    q = queries(2, kv, "bf16", 7)
+    clean, _ = attend_and_compare(c, kv, q, lens, "bf16")
+    status = new_status()
+    out, _ = M.moe_attn_decode(kv, q.cuda(), i32([2 ** 31 - 1, -5]), c.table.cuda(), c.k.cuda(), c.v.cuda(), status=status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [1, 0, 0, 0] and torch.equal(out[0], clean[0]) and (out[1] == 0).all()
+    for bad in (2, -2, 2 ** 31 - 1, -2 ** 31):
+        status = new_status()
+        out, lse = M.moe_attn_decode(kv, q.cuda(), i32(lens), c.table.cuda(), c.k.cuda(), c.v.cuda(), table_row=i32([0, bad]), want_lse=True, status=status)
+        torch.cuda.synchronize()
+        assert status.tolist() == [1, 0, 0, 0] and torch.equal(out[0], clean[0]) and (out[1] == 0).all() and (lse[1] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_offsets_beyond_32_bits(dtype):
+    # a cache of 9 GB each for K and V, the pages at its end
+    D, n_kv, P = 128, 8, 16
+    pool = (9 << 30) // (n_kv * P * D * (2 if dtype == "bf16" else 4))
+    lens = [500, 37]
+    small = Cache(lens, n_kv, D, P, dtype, 3)
+    kv = M.make_kv_shape(16, n_kv, D, P, small.table.shape[1], pool, dtype)
+    k, v = (torch.empty(kv.cache_shape, dtype=DT[dtype], device="cuda") for _ in range(2))
+    at = pool - small.k.shape[0]
+    k[at:], v[at:] = small.k.cuda(), small.v.cuda()
+    small.table[small.table >= 0] += at
+    attend_and_compare(small, kv, queries(2, kv, dtype, 1), lens, dtype, dev=(small.table.cuda(), k, v))
+    # and the write of a token there
+    x = torch.randn((1, (16 + 16) * D), generator=torch.Generator().manual_seed(1))
+    slot = (pool - 1) * P + 5
+    M.moe_qk_norm_rope(kv, x.cuda(), torch.zeros(0, dtype=torch.float64, device="cuda"), i32([0]), i32([slot]), k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(k[pool - 1, :, 5].cpu(), x[0, 16 * D:24 * D].view(8, D).to(DT[dtype]))
+    assert torch.equal(v[pool - 1, :, 5].cpu(), x[0, 24 * D:].view(8, D).to(DT[dtype]))
+
+
+def test_attention_one_workspace_for_calls_of_different_shapes():
+    big = M.make_kv_shape(48, 1, 256, 16, 600, 700, "f32")
+    ws = M.AttnWorkspace(big, 64)
+    for i, (lens, n_q, n_kv, D, dtype) in enumerate([([5000], 4, 1, 64, "bf16"), ([100, 3000, 9], 48, 1, 256, "f32"), ([9000], 8, 8, 32, "bf16"), ([1], 4, 2, 128, "bf16"),
+                                                     ([5000], 4, 1, 64, "bf16")]):
+        c = Cache(lens, n_kv, D, 16, dtype, i)
+        kv = M.make_kv_shape(n_q, n_kv, D, 16, c.table.shape[1], c.k.shape[0], dtype)
+        if ws.buf.numel() < M.attn_workspace_bytes(kv, len(lens)):
+            with pytest.raises(M.MoEError):
+                M.moe_attn_decode(kv, queries(len(lens), kv, dtype, i).cuda(), i32(lens), c.table.cuda(), c.k.cuda(), c.v.cuda(), workspace=ws)
+            continue
+        attend_and_compare(c, kv, queries(len(lens), kv, dtype, i), lens, dtype, workspace=ws)
+        assert (ws.buf[:16384] == 0).all()
+
+
+def test_attention_on_another_stream_and_in_a_graph():
+    lens = [3000, 17, 800, 0, 5]
+    c = Cache(lens, 2, 128, 16, "bf16", 11)
+    kv = M.make_kv_shape(8, 2, 128, 16, c.table.shape[1] + 1, c.k.shape[0], "bf16")
+    table = torch.cat([c.table, torch.full((5, 1), -1, dtype=torch.int32)], 1).cuda()
+    k, v, q = c.k.cuda(), c.v.cuda(), queries(5, kv, "bf16", 1).cuda()
+    seq = i32(lens)
+    want, want_lse = M.moe_attn_decode(kv, q, seq, table, k, v, want_lse=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        out, lse = M.moe_attn_decode(kv, q, seq, table, k, v, want_lse=True, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    # a graph of the three calls of a step: tables, norm and rotation, attention; lengths differ from replay to replay
+    x = torch.randn((5, (8 + 4) * 128), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    freq = torch.tensor([0.5, 0.01, 0.3, 0.001], dtype=torch.float64, device="cuda")
+    cached, fresh, free, head = seq.clone(), i32([1, 1, 0, 1, 1]), i32(np.setdiff1d(np.arange(c.k.shape[0]), c.table.numpy().ravel())), i32([0])
+    step, ws, out = M.KvStep(kv, 5, 4), M.AttnWorkspace(kv, 4), torch.empty((4, 8, 128), dtype=torch.bfloat16, device="cuda")
+    qs = torch.empty((4, 8, 128), dtype=torch.bfloat16, device="cuda")
+
+    def chain():
+        M.moe_kv_assign(kv, cached, fresh, free, head, table, step=step)
+        M.moe_qk_norm_rope(kv, x[:4], freq, step.positions, step.slots, k, v, q=qs)
+        M.moe_attn_decode(kv, qs, step.positions + 1, table, k, v, table_row=step.request, out=out, workspace=ws)
+
+    chain()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for i in range(4):
+        cached[0] -= 700                                   # shorter, so another split of the rows
+        x.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), qs.clone(), step.buf.clone()
+        out.zero_()
+        qs.zero_()
+        chain()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out) and torch.equal(got[1], qs) and torch.equal(got[2], step.buf) and out.abs().sum() > 0
+
+
+# ---------------------------------------------------------------------------- the three together
+
+@pytest.mark.parametrize("dtype,pairs", [("bf16", False), ("f32", True)])
+def test_prompts_and_decode_steps_end_to_end(dtype, pairs):
+    """Prompts of three requests, then single tokens, through tables, norm and rotation, and attention; the oracle keeps the
+    whole history in the rounded form that the cache has."""
+    n_q, n_kv, D, P, width, pool = 6, 2, 64, 4, 12, 40
+    kv = M.make_kv_shape(n_q, n_kv, D, P, width, pool, dtype)
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.full(kv.cache_shape, float("nan"), dtype=DT[dtype], device="cuda") for _ in range(2))
+    table = torch.full((3, width), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(pool, generator=g).to(torch.int32).cuda()
+    freq = torch.tensor([1000.0 ** (-i / 32) for i in range(32)], dtype=torch.float64).cuda()
+    gq, gk = (1.0 + 0.1 * torch.randn((D,), generator=g).cuda().cpu() for _ in range(2))
+    cached, head = i32([0, 0, 0]), i32([0])
+    history = [[np.zeros((0, n_kv, D)), np.zeros((0, n_kv, D))] for _ in range(3)]
+    for n, fresh in enumerate([[9, 1, 0], [1, 1, 14], [1, 0, 1], [1, 1, 1], [3, 1, 2]]):
+        T = sum(fresh)
+        step = M.moe_kv_assign(kv, cached, i32(fresh), free, head, table, T=T)
+        x = torch.randn((T, (n_q + 2 * n_kv) * D), generator=g)
+        q = M.moe_qk_norm_rope(kv, x.cuda(), freq, step.positions, step.slots, k, v, gq.cuda(), gk.cuda(), pairs=pairs)
+        out, _ = M.moe_attn_decode(kv, q, step.positions + 1, table, k, v, table_row=step.request)
+        torch.cuda.synchronize()
+        pos, req = step.positions.cpu().numpy(), step.request.cpu().numpy()
+        heads = f64(x).reshape(T, -1, D)
+        want_k, bound_k = attention.qk_norm_rope(heads[:, n_q:n_q + n_kv], f64(gk), 1e-5, freq.cpu().numpy(), pos, pairs)
+        slot = step.slots.cpu().numpy()
+        got_k, got_v = f64(k)[slot // P, :, slot % P], f64(v)[slot // P, :, slot % P]
+        within(got_k, want_k, bound_k, dtype, f"step {n} keys")
+        for b in range(3):
+            mine = req == b
+            history[b] = [np.concatenate([history[b][0], got_k[mine]]), np.concatenate([history[b][1], got_v[mine]])]
+        ref, bound = np.zeros((T, n_q, D)), np.zeros((T, n_q, D))
+        for r in range(T):
+            ks, vs = history[req[r]]
+            assert len(ks) > pos[r]
+            for h in range(n_kv):
+                hs = slice(h * 3, h * 3 + 3)
+                ref[r, hs], _, bound[r, hs], _ = attention.attend(f64(q)[r, hs], ks[:pos[r] + 1, h], vs[:pos[r] + 1, h], D ** -0.5, dtype == "bf16")
+        within(f64(out), ref, bound, dtype, f"step {n} attention")
+        cached, head = step.seq_len, step.free_head
+
+
+def test_errors_reach_the_caller():
+    kv = M.make_kv_shape(4, 2, 64, 16, 4, 10, "bf16")
+    k = torch.zeros(kv.cache_shape, dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    table, seq = torch.zeros((2, 4), dtype=torch.int32, device="cuda"), i32([1, 1])
+    with pytest.raises(ValueError, match="k_cache"):
+        M.moe_attn_decode(kv, q, seq, table, k[:5], k)
+    with pytest.raises(TypeError, match="k_cache"):
+        M.moe_attn_decode(kv, q, seq, table, k.float(), k)
+    with pytest.raises(ValueError, match="contiguous"):
+        M.moe_attn_decode(kv, q.transpose(0, 1).contiguous().transpose(0, 1), seq, table, k, k)
+    with pytest.raises(ValueError, match="seq_len"):
+        M.moe_attn_decode(kv, q, i32([1]), table, k, k)
+    with pytest.raises(M.MoEError) as e:
+        M.moe_attn_decode(kv, q, seq, table, k, k, window=-1)
+    assert e.value.status == B.ERR_INVALID_ARG
+    with pytest.raises(M.MoEError) as e:
+        M.moe_qk_norm_rope(kv, torch.zeros((2, 512), device="cuda"), torch.zeros(3, dtype=torch.float64, device="cuda"), seq, seq, k, k.clone())
+    assert e.value.status == B.ERR_INVALID_ARG                        # six elements: not a multiple of eight
+    with pytest.raises(M.MoEError):
+        M.moe_qk_norm_rope(kv, torch.zeros((2, 512), device="cuda"), torch.zeros(4, dtype=torch.float64, device="cuda"), seq, seq, k, k)      # one cache for both
+    out, _ = M.moe_attn_decode(kv, q[:0], seq[:0], table, k, k)
+    assert out.shape == (0, 4, 64)
