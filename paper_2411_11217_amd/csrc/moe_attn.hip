@@ -159,6 +159,26 @@ __device__ __forceinline__ void store_row(char* p, int r, const uint32_t (&v)[ND
 // maxima [H] and sums [H].
 constexpr int part_floats(int D, int H) { return H * (D + 2) + (-(H * (D + 2)) & 3); }
 
+// Partial results in the workspace are written by one XCD and read by another in the same launch.  Each XCD has an L2 of its own, and
+// a fence that makes plain stores visible writes back, one that makes plain loads current throws away, all of it: with fences
+// 256 requests took 707 us, 61 with a window 438.  These go past the L2 instead, as atomic accesses of device
+// scope, eight bytes each; what orders them is the wait for the stores before the counter goes up.
+__device__ __forceinline__ void put_far(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get_far(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+struct Halves { uint64_t lo, hi; };
+__device__ __forceinline__ void put_far(f32x4* p, f32x4 v) {
+    const Halves h = __builtin_bit_cast(Halves, v);
+    __hip_atomic_store((uint64_t*)p, h.lo, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store((uint64_t*)p + 1, h.hi, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4 get_far(const f32x4* p) {
+    Halves h;
+    h.lo = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    h.hi = __hip_atomic_load((const uint64_t*)p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return __builtin_bit_cast(f32x4, h);
+}
+__device__ __forceinline__ void far_stores_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 struct Split {                                   // a row that a wavefront shares with others
     int row, start, tiles;                       // row -1: none; tiles from `start` on
     int ends;                                    // this part has the row's last tile
@@ -492,10 +512,10 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(const AttnArgs a) {
                 if (a.lse && item < H) a.lse[(int64_t)first.row * a.n_q + head0 + rr] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
             } else {
 #pragma unroll
-                for (int j = 0; j < EPD; ++j) reinterpret_cast<f32x4*>(global)[(d * EPD + j) * 4 * H + c] = v[j];
+                for (int j = 0; j < EPD; ++j) put_far(reinterpret_cast<f32x4*>(global) + (d * EPD + j) * 4 * H + c, v[j]);
                 if (item < H) {
-                    global[H * D + rr] = top;
-                    global[H * D + H + rr] = sum;
+                    put_far(global + H * D + rr, top);
+                    put_far(global + H * D + H + rr, sum);
                 }
             }
         }
@@ -504,7 +524,7 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(const AttnArgs a) {
     }
 
     // ---- rows that several blocks share: the one that comes last joins them
-    __threadfence();
+    far_stores_done();
     __syncthreads();
     if (s_shared[0].row < 0 && s_shared[1].row < 0) return;
     int32_t* const counters = a.counters + (size_t)hx * a.runs;
@@ -520,7 +540,6 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(const AttnArgs a) {
     __syncthreads();
     for (int which = 0; which < 2; ++which) {
         if (!s_last[which]) continue;
-        __threadfence();
         const Split w = s_shared[which];
         const int run0 = w.start / share, n = (w.start + w.tiles - 1) / share - run0 + 1;
         const float* const chain = a.parts + ((size_t)hx * a.runs + run0) * 2 * part_room;     // part k: the second slot of run0, the first of the others
@@ -528,15 +547,15 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(const AttnArgs a) {
         float* const weight = s_parts;                       // [n][H]
         for (int h = wave; h < H; h += kWaves) {
             float top = -INFINITY, sum = 0.f;
-            for (int k = lane; k < n; k += 64) top = fmaxf(top, part_of(k)[H * D + h]);
+            for (int k = lane; k < n; k += 64) top = fmaxf(top, get_far(part_of(k) + H * D + h));
 #pragma unroll
             for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
             const float ref = top == -INFINITY ? 0.f : top;
-            for (int k = lane; k < n; k += 64) sum += __builtin_amdgcn_exp2f(part_of(k)[H * D + h] - ref) * part_of(k)[H * D + H + h];
+            for (int k = lane; k < n; k += 64) sum += __builtin_amdgcn_exp2f(get_far(part_of(k) + H * D + h) - ref) * get_far(part_of(k) + H * D + H + h);
 #pragma unroll
             for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 64);
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            for (int k = lane; k < n; k += 64) weight[k * H + h] = __builtin_amdgcn_exp2f(part_of(k)[H * D + h] - ref) * inv;
+            for (int k = lane; k < n; k += 64) weight[k * H + h] = __builtin_amdgcn_exp2f(get_far(part_of(k) + H * D + h) - ref) * inv;
             if (a.lse && lane == 0) a.lse[(int64_t)w.row * a.n_q + head0 + h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
         }
         __syncthreads();
@@ -548,10 +567,10 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(const AttnArgs a) {
 #pragma unroll 4
             for (int k = 0; k < n; ++k)
 #pragma unroll
-                for (int j = 0; j < EPD; ++j) v[j] += weight[k * H + rr] * reinterpret_cast<const f32x4*>(part_of(k))[(d * EPD + j) * 4 * H + c];
+                for (int j = 0; j < EPD; ++j) v[j] += weight[k * H + rr] * get_far(reinterpret_cast<const f32x4*>(part_of(k)) + (d * EPD + j) * 4 * H + c);
             write_item(item, w.row, v);
         }
-        if (threadIdx.x == 0) counters[run0] = 0;            // for the next call
+        if (threadIdx.x == 0) counters[run0] = 0;            // for the next call: nobody else of this one looks at it again
         __syncthreads();
     }
 }
