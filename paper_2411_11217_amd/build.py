@@ -22,6 +22,10 @@ FLAGS = [
     "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
+# The accumulators of this file's MFMAs are rescaled by vector instructions in every tile: in accumulator registers, the
+# compiler's choice, each would be copied out and back (32 registers both ways per tile for heads of 128).
+FILE_FLAGS = {"moe_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-pthread", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
@@ -84,7 +88,7 @@ def build(force: bool = True, verbose: bool = False, extra_flags=(), out: str = 
         if src.endswith(".cpp"):
             cmd = [os.environ.get("CXX", "g++")] + HOST_FLAGS + ["-c", src, "-o", obj]
         else:
-            cmd = [hipcc] + FLAGS + list(extra_flags) + (["-save-temps=obj"] if checked else []) + ["-c", src, "-o", obj]
+            cmd = [hipcc] + FLAGS + FILE_FLAGS.get(os.path.basename(src), []) + list(extra_flags) + (["-save-temps=obj"] if checked else []) + ["-c", src, "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True, cwd=build_dir)
         if r.returncode != 0:
             raise RuntimeError("compiler failed for %s:\n%s" % (src, r.stderr[-8000:]))
