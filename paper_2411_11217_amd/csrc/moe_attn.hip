@@ -22,6 +22,7 @@
 //   bf16: 32 tokens are the 32 steps of one 16x16x32 MFMA.  The weights are split into two bf16 parts, 16 bits of each weight: half
 // a bf16 step on the weights would show in the outputs.  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded.
 #include <algorithm>
+#include <type_traits>
 
 #include "moe_internal.h"
 
@@ -219,7 +220,10 @@ template <class Elem, int D, bool ONCE>
 __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const AttnArgs a) {
     constexpr int TILE = Kind<Elem>::kTile, SUB = TILE / 16, EPD = Kind<Elem>::kPerDword;
     constexpr int ROW_BYTES = D * (int)sizeof(Elem), KS = ROW_BYTES / 64, ND = ROW_BYTES / 64, E = D / 16;
-    constexpr int PITCH = ROW_BYTES + 16;                    // of a row of keys in LDS
+    constexpr int PITCH = ROW_BYTES + 16, CHUNKS = ROW_BYTES / 16, KN = TILE * CHUNKS / 64;      // of a tile in LDS; chunks of a row, loads of a tile
+    // us for 64 requests of 500 to 5000 tokens, 8 key/value heads, bf16, rows one by one / 16 bytes at a time: heads of 64 60 / 55, 96: 82 / 76,
+    // 160: 119 / 126 (which takes the registers of a second block).
+    constexpr bool BY_ROWS = ROW_BYTES >= 256;
     extern __shared__ __align__(16) float s_parts[];         // of each wavefront wave_floats; in the last join join_floats
     __shared__ int s_before[kThreads];
     __shared__ int s_sum[kWaves];
@@ -349,24 +353,47 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             places[lane & (TILE - 1)] = (page * (uint32_t)a.n_kv + (uint32_t)kv) * (uint32_t)a.P + (uint32_t)(t - p * a.P);
         };
         char* const keys = reinterpret_cast<char*>(slot_of(wave * 2 + 1));
-        uint32_t kr[TILE / 4][ND];
+        using Held = std::conditional_t<BY_ROWS, uint32_t[TILE / 4][ND], u32x4[KN]>;
+        Held kr;
+        [[maybe_unused]] Held vr;                            // if not BY_ROWS, until the keys have left the LDS
         u32x4 qf[KS];
-        uint32_t vf[SUB][4][ND];
-        // Keys come as whole cache lines, chunk by chunk of 16 bytes, and get to the lanes of the MFMA through the wavefront's own LDS:
-        // 16 rows x 64 bytes per load, as the MFMA has them, are half lines, and 256 requests took 4 % longer, a window 12 %.
-        auto load_k = [&]() __attribute__((always_inline)) {
+        uint32_t vf[SUB][4][ND];                             // of token u * 16 + 4 g + i, the dwords of lane r
+        // Keys come as whole cache lines and get to the lanes of the MFMA through the wavefront's own LDS: 16 rows x 64 bytes per load,
+        // as the MFMA has them, are half lines, and 256 requests took 4 % longer, a window 12 %.  Where a row has less than 256 bytes, a
+        // load takes 64 chunks of 16 bytes in a row, across its rows, of the values too (not BY_ROWS).
+        auto load_tile = [&](const char* from, Held& v) __attribute__((always_inline)) {
+            if constexpr (BY_ROWS) {
 #pragma unroll
-            for (int k = 0; k < TILE / 4; ++k) load_row<ND, ONCE>(a.k + (uint64_t)places[g * (TILE / 4) + k] * ROW_BYTES, r, kr[k]);
+                for (int k = 0; k < TILE / 4; ++k) load_row<ND, ONCE>(from + (uint64_t)places[g * (TILE / 4) + k] * ROW_BYTES, r, v[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < KN; ++k) {
+                    const int i = k * 64 + lane, t = i / CHUNKS;
+                    v[k] = load16<ONCE>(from + (uint64_t)places[t] * ROW_BYTES + (i - t * CHUNKS) * 16);
+                }
+            }
         };
-        auto stage_k = [&]() __attribute__((always_inline)) {
+        auto stage_tile = [&](const Held& v) __attribute__((always_inline)) {
+            if constexpr (BY_ROWS) {
 #pragma unroll
-            for (int k = 0; k < TILE / 4; ++k) store_row<ND>(keys + (g * (TILE / 4) + k) * PITCH, r, kr[k]);
+                for (int k = 0; k < TILE / 4; ++k) store_row<ND>(keys + (g * (TILE / 4) + k) * PITCH, r, v[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < KN; ++k) {
+                    const int i = k * 64 + lane, t = i / CHUNKS;
+                    *reinterpret_cast<u32x4*>(keys + t * PITCH + (i - t * CHUNKS) * 16) = v[k];
+                }
+            }
         };
         auto load_v = [&]() __attribute__((always_inline)) {
+            if constexpr (BY_ROWS) {
 #pragma unroll
-            for (int u = 0; u < SUB; ++u)
+                for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) load_row<ND, ONCE>(a.v + (uint64_t)places[u * 16 + g * 4 + i] * ROW_BYTES, r, vf[u][i]);
+                    for (int i = 0; i < 4; ++i) load_row<ND, ONCE>(a.v + (uint64_t)places[u * 16 + g * 4 + i] * ROW_BYTES, r, vf[u][i]);
+            } else {
+                load_tile(a.v, vr);
+            }
         };
         auto load_q = [&](int row) __attribute__((always_inline)) {
             const char* p = a.q + ((int64_t)row * a.n_q + head0 + min(r, H - 1)) * ROW_BYTES + g * 16;
@@ -383,7 +410,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         int from = x0;                                       // the first tile of the current row that is this wavefront's
         place(now);
         load_q(now.row);
-        load_k();
+        load_tile(a.k, kr);
         load_v();
         Now nxt = now;
         if (x0 + 1 < x1) {
@@ -392,8 +419,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         }
         auto tile = [&](int x, auto more_c) __attribute__((always_inline)) {
             constexpr bool more = decltype(more_c)::value;
-            stage_k();
-            if (more) load_k();
+            stage_tile(kr);
+            if (more) load_tile(a.k, kr);
             f32x4 sc[SUB];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
@@ -438,6 +465,13 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                     sc[u][i] = __builtin_amdgcn_exp2f(sc[u][i] - ref);
                     l += sc[u][i];
                 }
+            if constexpr (!BY_ROWS) {
+                stage_tile(vr);
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) load_row<ND, false>(keys + (u * 16 + g * 4 + i) * PITCH, r, vf[u][i]);
+            }
             if (!whole) {                                    // weight 0 times whatever the repeated token holds is not always 0
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
