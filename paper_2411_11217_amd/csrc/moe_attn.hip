@@ -45,7 +45,7 @@ struct AttnArgs {
     int32_t* counters;
     float* parts;
     int32_t* status;
-    uint64_t page_magic;                         // t / P == t * page_magic >> page_shift for 0 <= t < 2^31
+    uint64_t page_magic;
     int page_shift;
     int R, n_q, n_kv, group, head_tiles, P, max_pages, table_rows, window, runs;
     uint32_t pool_pages;
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         // read the ones they load from LDS, four at a time (one cross-lane move for each took as long as the rest of the tile).
         auto place = [&](const Now& w) __attribute__((always_inline)) {
             const int t = max(min(w.t0 + (lane & (TILE - 1)), w.len - 1), w.first);
-            const int p = (int)(((uint64_t)(uint32_t)t * a.page_magic) >> a.page_shift);
+            const int p = divide(t, a.page_magic, a.page_shift);
             uint32_t page = (uint32_t)a.block_table[(int64_t)w.table * a.max_pages + p];
             if (page >= a.pool_pages) {
                 if (w.len > 0) flags |= 1;
@@ -713,8 +713,6 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
     }
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 // The launch: `runs` blocks for each key/value head and 16 of its query heads.
 struct Plan {
     int head_tiles, runs;
@@ -814,10 +812,7 @@ int moe_attn_decode(const moe_kv_shape* s, int32_t R, const void* q, const int32
     a.counters = (int32_t*)workspace;
     a.parts = (float*)((char*)workspace + MOE_ATTN_COUNTER_BYTES);
     a.status = status;
-    int bits = 0;
-    while (((int64_t)1 << bits) < s->page_tokens) ++bits;
-    a.page_shift = 31 + bits;
-    a.page_magic = ((uint64_t)1 << a.page_shift) / (uint64_t)s->page_tokens + 1;       // 33 bits at most; the error times 2^31 stays below 2^page_shift
+    a.page_magic = division_magic(s->page_tokens, a.page_shift);
     a.R = R;
     a.n_q = s->n_q;
     a.n_kv = s->n_kv;

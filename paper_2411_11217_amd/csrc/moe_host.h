@@ -51,6 +51,17 @@ int64_t linear_pages(const moe_linear_shape& s);
 // Attention over a paged cache: MOE_OK or an error.
 int validate_kv(const moe_kv_shape* s);
 
+// t / d == t * magic >> shift for 0 <= t < 2^31 and 1 <= d < 2^31: with 2^(bits - 1) < d <= 2^bits and shift = 31 + bits the magic is
+// floor(2^shift / d) + 1 <= 2^32 (d = 1: 2^31 + 1), magic * d - 2^shift is in (0, d], and t times that stays below 2^shift.
+inline uint64_t division_magic(int32_t d, int& shift) {
+    int bits = 0;
+    while (((int64_t)1 << bits) < d) ++bits;
+    shift = 31 + bits;
+    return ((uint64_t)1 << shift) / (uint64_t)d + 1;
+}
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
 // Where the dense linear map takes the kernel for few rows (csrc/moe_ffn_rows_bf16.hip): as long as blocks of 64 columns and 128
 // rows, or with more than 128 rows of 128 columns and 64 rows, make one round on the 256 compute units (which blocks it has
 // then is linear_rows_block's choice), and with a short k and few rows.

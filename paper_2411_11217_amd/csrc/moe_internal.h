@@ -35,6 +35,9 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
     return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;                        // round to nearest, ties to even
 }
 
+// t / d for 0 <= t < 2^31, with the magic and the shift of division_magic(d, shift).
+__device__ __forceinline__ int divide(int t, uint64_t magic, int shift) { return (int)(((uint64_t)(uint32_t)t * magic) >> shift); }
+
 // ---- kernel launchers (each returns MOE_OK or MOE_ERR_HIP) -----------------
 // What the permutation writes (moe_permute of the C ABI, without the copy of x).
 struct PlaceOut {

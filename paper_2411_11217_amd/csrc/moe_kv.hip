@@ -9,59 +9,52 @@ using namespace moe;
 namespace {
 
 // ---- block tables and slot maps ---------------------------------------------------
-// Two prefix sums over the requests (rows, new pages), then every row, page and request finds its place by itself.  One
-// launch: every block forms both sums from the counts (at most 4096 requests, 32 KB) and serves the rows it strides over;
-// a launch for the sums alone would cost more than all of it.
-constexpr int kAssignThreads = 256;
+// Two prefix sums over the requests (rows, new pages), then every row, page and request finds its place by itself, with a
+// search in the sums.  One launch: every block forms both sums from the counts (at most 4096 requests, 32 KB that come from
+// the L2) and serves the rows it strides over; a launch for the sums alone would cost more.  A call writes 12 bytes per row; it is bound by
+// the latency of its chain (counts, two sums, page, slot) up to some 100000 rows.  us, in a graph: 36 requests of one token ASSIGN1, 128 prompts
+// of 18600 tokens ASSIGN2, 4000 requests of 450000 rows ASSIGN3.
 constexpr uint32_t kManyRows = 1u << 30;         // sums stop here: nothing that large is ever served
+constexpr uint32_t kServed = 1u << 31;           // beside a sum of pages
 
 struct AssignArgs {
     const int32_t *cached, *fresh, *free_pages, *free_head;
     int32_t *block_table, *seq_len, *row_start, *positions, *slots, *request, *free_head_out, *status;
-    int B, T, P, max_pages, n_free;
-    int64_t pool_pages;
+    uint64_t page_magic;
+    int page_shift;
+    int B, T, P, max_pages, n_free, vectors;     // vectors: positions, slots and request are 16-byte aligned
+    uint32_t pool_pages;
 };
 
-struct Wants {                                   // what a request asks for
-    int cached, held, need;                      // tokens and pages it has, new pages
-    bool bad, fits;                              // a negative count; not bad, and rows and pages have room
-};
+// Pages of n tokens.
+__device__ __forceinline__ int pages_of(const AssignArgs& a, int n) { return n > 0 ? divide(n - 1, a.page_magic, a.page_shift) + 1 : 0; }
 __device__ __forceinline__ uint32_t rows_of(int fresh, int T) { return (uint32_t)min(max(fresh, 0), T + 1); }
-__device__ __forceinline__ Wants wants(const AssignArgs& a, int b, uint32_t row) {
-    Wants w;
-    const int c = a.cached[b], f = a.fresh[b];
-    w.bad = c < 0 || f < 0;
-    w.cached = max(c, 0);
-    w.held = (int)(((int64_t)w.cached + a.P - 1) / a.P);
-    const int64_t pages = ((int64_t)w.cached + max(f, 0) + a.P - 1) / a.P;
-    w.fits = !w.bad && (uint64_t)row + (uint32_t)f <= (uint32_t)a.T && pages <= a.max_pages;
-    w.need = w.fits ? (int)pages - w.held : 0;
-    return w;
-}
 __device__ __forceinline__ uint32_t add_rows(uint32_t x, uint32_t y) { return min(x + y, kManyRows); }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t add_moved(uint32_t v) { return add_rows(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false)); }
+
 // The sum over the threads before this one, and over all of them.  part: one word per wavefront.
+template <int THREADS>
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* part, uint32_t& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t incl = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t u = __shfl_up(incl, d, 64);
-        if (lane >= d) incl = add_rows(incl, u);
-    }
-    uint32_t before = __shfl_up(incl, 1, 64);
-    if (lane == 0) before = 0;
-    __syncthreads();
+    uint32_t incl = add_moved<0x111, 0xf>(v);    // one lane up in rows of 16, then two, four, eight, from row to row, from half to half
+    incl = add_moved<0x112, 0xf>(incl);
+    incl = add_moved<0x114, 0xf>(incl);
+    incl = add_moved<0x118, 0xf>(incl);
+    incl = add_moved<0x142, 0xa>(incl);
+    incl = add_moved<0x143, 0xc>(incl);
     if (lane == 63) part[wave] = incl;
+    uint32_t run = __shfl_up(incl, 1, 64);       // saturated sums cannot be taken apart again
+    if (lane == 0) run = 0;
     __syncthreads();
-    uint32_t run = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kAssignThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) run = add_rows(run, part[w]);
         total = add_rows(total, part[w]);
     }
-    return add_rows(run, before);
+    return run;
 }
 
 // The last of n ascending sums that is at most v; the first is 0.
@@ -69,85 +62,140 @@ __device__ __forceinline__ int last_at_most(const uint32_t* sums, int n, uint32_
     int lo = 0, hi = n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (sums[mid] <= v) lo = mid;
+        if ((sums[mid] & ~kServed) <= v) lo = mid;
         else hi = mid;
     }
     return lo;
 }
 
-__global__ __launch_bounds__(kAssignThreads) void assign_kernel(const AssignArgs a) {
-    extern __shared__ uint32_t sums[];           // [B] rows before a request, [B] new pages before it
-    __shared__ uint32_t part[kAssignThreads / 64];
-    __shared__ uint32_t s_used;
-    uint32_t* row0 = sums;
-    uint32_t* page0 = sums + a.B;
-    const int per = (a.B + kAssignThreads - 1) / kAssignThreads;
-    const int b0 = min((int)threadIdx.x * per, a.B), b1 = min(b0 + per, a.B);
+// PER requests to a thread: B <= THREADS * PER.
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a) {
+    extern __shared__ uint32_t sums[];           // [B] rows before a request, [B] new pages before it and whether it is served
+    __shared__ uint32_t row_part[THREADS / 64], page_part[THREADS / 64], s_used;
+    uint32_t* const row0 = sums;
+    uint32_t* const page0 = sums + a.B;
+    const int b0 = threadIdx.x * PER;
+    const uint32_t T = (uint32_t)a.T;
+    if (threadIdx.x == 0) s_used = 0;
     const int head = a.free_head[0];
+    int cached[PER], fresh[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        cached[j] = b0 + j < a.B ? a.cached[b0 + j] : 0;
+        fresh[j] = b0 + j < a.B ? a.fresh[b0 + j] : 0;
+    }
     const bool head_ok = head >= 0 && head <= a.n_free;
     const uint32_t left = head_ok ? (uint32_t)(a.n_free - head) : 0;
-    if (threadIdx.x == 0) s_used = 0;
-
-    uint32_t rows = 0, total_rows, total_pages;
-    for (int b = b0; b < b1; ++b) rows = add_rows(rows, rows_of(a.fresh[b], a.T));
-    uint32_t row = block_scan(rows, part, total_rows);
-    uint32_t pages = 0;
-    for (int b = b0; b < b1; ++b) {
-        row0[b] = row;
-        pages = add_rows(pages, (uint32_t)wants(a, b, row).need);
-        row = add_rows(row, rows_of(a.fresh[b], a.T));
-    }
-    uint32_t page = block_scan(pages, part, total_pages);
-    uint32_t used = 0;
     int flags = head_ok ? 0 : 1;
-    for (int b = b0; b < b1; ++b) {
-        const Wants w = wants(a, b, row0[b]);
-        page0[b] = page;
-        page = add_rows(page, (uint32_t)w.need);
-        const bool served = w.fits && (w.need == 0 || page <= left);
-        if (served && w.need) used = page;
-        if (!served) flags |= w.bad ? 1 : (uint64_t)row0[b] + (uint32_t)a.fresh[b] > (uint32_t)a.T ? 4 : 2;
+
+    uint32_t rows = 0, pages = 0, total_rows, total_pages, row[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) rows = add_rows(rows, rows_of(fresh[j], a.T));
+    rows = block_scan<THREADS>(rows, row_part, total_rows);
+    int need[PER];
+    bool fits[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        row[j] = rows;
+        if (b0 + j < a.B) row0[b0 + j] = rows;
+        rows = add_rows(rows, rows_of(fresh[j], a.T));
+        const bool bad = cached[j] < 0 || fresh[j] < 0, room = rows <= T;
+        // cached + fresh <= max_pages * P < 2^31 where the pages fit
+        const bool held = !bad && (uint32_t)cached[j] + (uint32_t)fresh[j] <= (uint32_t)(a.max_pages * a.P);
+        fits[j] = held && room;
+        need[j] = fits[j] ? pages_of(a, cached[j] + fresh[j]) - pages_of(a, cached[j]) : 0;
+        pages = add_rows(pages, (uint32_t)need[j]);
+        if (!fits[j]) flags |= bad ? 1 : !room ? 4 : 2;
+    }
+    pages = block_scan<THREADS>(pages, page_part, total_pages);
+    uint32_t used = 0;
+    bool served[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const uint32_t before = pages;
+        pages = add_rows(pages, (uint32_t)need[j]);
+        served[j] = fits[j] && (need[j] == 0 || pages <= left);
+        if (served[j] && need[j]) used = pages;
+        if (fits[j] && !served[j]) flags |= 2;
+        if (b0 + j < a.B) page0[b0 + j] = before | (served[j] ? kServed : 0);
     }
     if (used) atomicMax(&s_used, used);
+    if (blockIdx.x == 0) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (b0 + j < a.B) {
+                a.seq_len[b0 + j] = served[j] ? cached[j] + fresh[j] : max(cached[j], 0);
+                a.row_start[b0 + j] = (int)min(row[j], T);
+            }
+        if (flags && a.status) atomicOr(a.status, flags);
+    }
+    flags = 0;
     __syncthreads();
+    const uint32_t live = min(total_rows, T), n_pages = s_used;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        a.row_start[a.B] = (int)live;
+        a.free_head_out[0] = head + (int)n_pages;
+    }
 
-    const uint32_t T = (uint32_t)a.T;
-    const uint32_t live = min(total_rows, T);
-    const uint32_t n = max(max(T, (uint32_t)a.B + 1), min(total_pages, left));
-    for (uint32_t i = blockIdx.x * kAssignThreads + threadIdx.x; i < n; i += gridDim.x * kAssignThreads) {
-        if (i < T) {
-            int pos = 0, slot = -1, req = -1;
-            if (i < live) {
-                req = last_at_most(row0, a.B, i);
-                const Wants w = wants(a, req, row0[req]);
-                pos = (int)min((int64_t)w.cached + (i - row0[req]), (int64_t)INT32_MAX);
-                if (w.fits && (w.need == 0 || page0[req] + (uint32_t)w.need <= left)) {
-                    const int p = pos / a.P;
-                    const int got = p < w.held ? a.block_table[(size_t)req * a.max_pages + p] : a.free_pages[head + (int)page0[req] + p - w.held];
-                    if (got >= 0 && got < a.pool_pages) slot = got * a.P + (pos - p * a.P);
+    const uint32_t step = gridDim.x * THREADS, me = blockIdx.x * THREADS + threadIdx.x;
+    for (uint32_t i = me; i < n_pages; i += step) {          // all of them are served requests'
+        const int b = last_at_most(page0, a.B, i);
+        a.block_table[(size_t)b * a.max_pages + pages_of(a, a.cached[b]) + (int)(i - (page0[b] & ~kServed))] = a.free_pages[head + (int)i];
+    }
+    for (uint32_t i = me * 4; i < T; i += step * 4) {        // four rows at a time, one search for them
+        int pos[4] = {0, 0, 0, 0}, slot[4] = {-1, -1, -1, -1}, req[4] = {-1, -1, -1, -1};
+        if (i < live) {
+            int b = last_at_most(row0, a.B, i), of = -1, last_page = -1, page = -1;
+            int had = 0, held = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i + j >= live) continue;
+                while (b + 1 < a.B && row0[b + 1] <= i + j) ++b;
+                if (b != of) {
+                    of = b;
+                    had = max(a.cached[b], 0);
+                    held = pages_of(a, had);
+                    last_page = -1;
+                }
+                req[j] = b;
+                pos[j] = (int)min((int64_t)had + (i + j - row0[b]), (int64_t)INT32_MAX);
+                const uint32_t before = page0[b];
+                if (before & kServed) {
+                    const int p = divide(pos[j], a.page_magic, a.page_shift);
+                    if (p != last_page) {
+                        last_page = p;
+                        page = p < held ? a.block_table[(size_t)b * a.max_pages + p] : a.free_pages[head + (int)(before & ~kServed) + p - held];
+                    }
+                    if ((uint32_t)page < a.pool_pages) slot[j] = page * a.P + (pos[j] - p * a.P);
                     else flags |= 1;
                 }
             }
-            a.positions[i] = pos;
-            a.slots[i] = slot;
-            a.request[i] = req;
         }
-        if (i < (uint32_t)a.B) {
-            const Wants w = wants(a, i, row0[i]);
-            const bool served = w.fits && (w.need == 0 || page0[i] + (uint32_t)w.need <= left);
-            a.seq_len[i] = served ? w.cached + a.fresh[i] : w.cached;
-            a.row_start[i] = (int)min(row0[i], T);
-        } else if (i == (uint32_t)a.B) {
-            a.row_start[i] = (int)live;
-            a.free_head_out[0] = head + (int)s_used;
-        }
-        if (i < min(total_pages, left)) {
-            const int b = last_at_most(page0, a.B, i);
-            const Wants w = wants(a, b, row0[b]);
-            if (page0[b] + (uint32_t)w.need <= left) a.block_table[(size_t)b * a.max_pages + w.held + (int)(i - page0[b])] = a.free_pages[head + (int)i];
+        if (a.vectors && i + 4 <= T) {
+            *reinterpret_cast<int4*>(a.positions + i) = int4{pos[0], pos[1], pos[2], pos[3]};
+            *reinterpret_cast<int4*>(a.slots + i) = int4{slot[0], slot[1], slot[2], slot[3]};
+            *reinterpret_cast<int4*>(a.request + i) = int4{req[0], req[1], req[2], req[3]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i + j < T) {
+                    a.positions[i + j] = pos[j];
+                    a.slots[i + j] = slot[j];
+                    a.request[i + j] = req[j];
+                }
         }
     }
     if (a.status && flags) atomicOr(a.status, flags);
+}
+
+template <int THREADS, int PER>
+int launch_assign(const AssignArgs& a, hipStream_t st) {
+    // a block for as many rows (four to a thread) as it has threads; beyond two blocks per compute unit they stride
+    const int blocks = (int)std::min<int64_t>(std::max<int64_t>(((int64_t)a.T + 4 * THREADS - 1) / (4 * THREADS), 1), 2 * 256 * 256 / THREADS);
+    hipLaunchKernelGGL((assign_kernel<THREADS, PER>), dim3(blocks), dim3(THREADS), (size_t)a.B * 8, st, a);
+    MOE_HIP_TRY(hipGetLastError());
+    return MOE_OK;
 }
 
 // ---- norm and rotation of queries and keys, the write into the cache --------------------------
@@ -265,8 +313,6 @@ int launch_rope(const RopeArgs& a, bool pairs, hipStream_t st) {
     return MOE_OK;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 }  // namespace
 
 extern "C" {
@@ -288,12 +334,28 @@ int moe_kv_assign(const moe_kv_shape* s, int32_t B, int32_t T, const int32_t* ca
     for (const auto& i : in)
         for (const auto& o : out)
             if (i.p && o.p && i.bytes && o.bytes && overlap(i.p, i.bytes, o.p, o.bytes)) return MOE_ERR_INVALID_ARG;
-    const AssignArgs a{cached, fresh, free_pages, free_head, block_table, seq_len, row_start, positions, slots, request, free_head_out, status,
-                       B, T, s->page_tokens, s->max_pages, n_free, s->pool_pages};
-    const int blocks = std::min((std::max(T, B + 1) + kAssignThreads - 1) / kAssignThreads, 1024);
-    hipLaunchKernelGGL(assign_kernel, dim3(blocks), dim3(kAssignThreads), (size_t)B * 8, (hipStream_t)stream, a);
-    MOE_HIP_TRY(hipGetLastError());
-    return MOE_OK;
+    AssignArgs a{};
+    a.cached = cached;
+    a.fresh = fresh;
+    a.free_pages = free_pages;
+    a.free_head = free_head;
+    a.block_table = block_table;
+    a.seq_len = seq_len;
+    a.row_start = row_start;
+    a.positions = positions;
+    a.slots = slots;
+    a.request = request;
+    a.free_head_out = free_head_out;
+    a.status = status;
+    a.page_magic = division_magic(s->page_tokens, a.page_shift);
+    a.B = B;
+    a.T = T;
+    a.P = s->page_tokens;
+    a.max_pages = s->max_pages;
+    a.n_free = n_free;
+    a.vectors = aligned16(positions) && aligned16(slots) && aligned16(request);
+    a.pool_pages = (uint32_t)s->pool_pages;
+    return B <= 256 ? launch_assign<256, 1>(a, (hipStream_t)stream) : launch_assign<1024, 4>(a, (hipStream_t)stream);
 }
 
 int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t qkv_dtype, int64_t row_elements,
