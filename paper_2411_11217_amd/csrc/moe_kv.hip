@@ -12,8 +12,8 @@ namespace {
 // Two prefix sums over the requests (rows, new pages), then every row, page and request finds its place by itself, with a
 // search in the sums.  One launch: every block forms both sums from the counts (at most 4096 requests, 32 KB that come from
 // the L2) and serves the rows it strides over; a launch for the sums alone would cost more.  A call writes 12 bytes per row; it is bound by
-// the latency of its chain (counts, two sums, page, slot) up to some 100000 rows.  us, in a graph: 36 requests of one token ASSIGN1, 128 prompts
-// of 18600 tokens ASSIGN2, 4000 requests of 450000 rows ASSIGN3.
+// the latency of its chain (counts, two sums, page, slot) up to some 100000 rows.  us, in a graph: 36 requests of one token 5.7, 128 prompts
+// of 18600 tokens 7.3, 4000 requests of 529000 rows 15.7.
 constexpr uint32_t kManyRows = 1u << 30;         // sums stop here: nothing that large is ever served
 constexpr uint32_t kServed = 1u << 31;           // beside a sum of pages
 
@@ -204,8 +204,9 @@ int launch_assign(const AssignArgs& a, hipStream_t st) {
 // part that is rotated by halves the vectors are elements 4 l .. and rot / 2 + 4 l .., the two sides of four pairs, so that a
 // rotation needs no other lane; elsewhere they are neighbours.  rot_dim is a multiple of 8, so no lane has both kinds.
 // The angle is formed in 64 bits as a number of turns, whose whole part falls away exactly: at position 10^6 a float
-// product would be off by 0.03 radians.
-constexpr int kRopeWaves = 4;
+// product would be off by 0.03 radians.  Every wavefront forms the four angles of its lanes once for all of its heads.  9857 rows of 48 + 2 * 8 heads
+// of 128, 484 MB: 83 us; a large copy moves 4.96 TB/s here.  256 rows of 32 + 2 * 8 heads 4.4 us, of which 2.9 are the launch.
+constexpr int kFewRows = 512;
 
 struct RopeArgs {
     const void* qkv;
@@ -215,102 +216,153 @@ struct RopeArgs {
     void *q, *k_cache, *v_cache;
     int32_t* status;
     int64_t row_elements, pool_tokens;
-    float eps;
+    uint64_t page_magic;
+    int page_shift;
+    float eps, per_element;
     int T, n_q, n_kv, D, P, rot, lph;
 };
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const uint16_t* p) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    return float4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+template <bool FAR, class V>
+__device__ __forceinline__ V load_as(const void* p) {
+    return FAR ? __builtin_nontemporal_load(reinterpret_cast<const V*>(p)) : *reinterpret_cast<const V*>(p);
 }
-__device__ __forceinline__ void store4(float* p, const float4& v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(uint16_t* p, const float4& v) {
-    uint2 o;
-    o.x = f32_to_bf16_bits(v.x) | (f32_to_bf16_bits(v.y) << 16);
-    o.y = f32_to_bf16_bits(v.z) | (f32_to_bf16_bits(v.w) << 16);
-    *reinterpret_cast<uint2*>(p) = o;
+template <bool FAR, class V>
+__device__ __forceinline__ void store_as(void* p, V v) {
+    if constexpr (FAR) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+    else *reinterpret_cast<V*>(p) = v;
+}
+template <bool FAR>
+__device__ __forceinline__ f32x4 load4(const float* p) { return load_as<FAR, f32x4>(p); }
+template <bool FAR>
+__device__ __forceinline__ f32x4 load4(const uint16_t* p) {
+    const u32x2 v = load_as<FAR, u32x2>(p);
+    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+}
+template <bool FAR>
+__device__ __forceinline__ void store4(float* p, f32x4 v) { store_as<FAR, f32x4>(p, v); }
+template <bool FAR>
+__device__ __forceinline__ void store4(uint16_t* p, f32x4 v) {
+    store_as<FAR, u32x2>(p, __builtin_bit_cast(u32x2, __builtin_convertvector(v, bf16x4)));       // to nearest even
 }
 
-template <class In, class Out, bool PAIRS>
-__global__ __launch_bounds__(kRopeWaves * 64) void qk_norm_rope_kernel(const RopeArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Sine and cosine of `turns` turns.  What is left of a quarter turn, up to 45 degrees either way, is small enough for the first terms of the
+// Taylor series: those left out are below 2 10^-9 (sine) and 3 10^-8 (cosine).
+__device__ __forceinline__ void sine_cosine(double turns, float& sine, float& cosine) {
+    const double quarters = (turns - rint(turns)) * 4.0, whole = rint(quarters);
+    const float x = (float)(quarters - whole) * 1.57079632679489661923f, x2 = x * x;
+    const float s = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), x);
+    const float c = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.f / 40320, -1.f / 720), 1.f / 24), -0.5f), 1.f);
+    const int q = (int)whole;
+    const float a = q & 1 ? c : s, b = q & 1 ? s : c;
+    sine = __uint_as_float(__float_as_uint(a) ^ ((uint32_t)(q & 2) << 30));
+    cosine = __uint_as_float(__float_as_uint(b) ^ ((uint32_t)((q + 1) & 2) << 30));
+}
+
+// A block has one row and WAVES wavefronts: with up to 512 rows (two blocks per compute unit) eight, for the latency, with more
+// four, and then neither side is kept in the caches (FAR).  us in a graph, 32 + 2 * 8 heads of 128, float32 in, bf16 out: 256 rows with
+// eight / four 4.5 / 5.4, 1000 rows 11.2 / 10.7, 9857 rows 80 / 75; with the hint 700 rows 8.8 / 7.3, 5000 rows 43 / 37, 9857 rows 76 / 68.
+template <class In, class Out, bool PAIRS, int WAVES, bool FAR>
+__global__ __launch_bounds__(WAVES * 64) void qk_norm_rope_kernel(const RopeArgs a) {
+    constexpr int AT_ONCE = 2;                               // groups of heads whose loads are under way together
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = blockIdx.x;
     const int l = lane & (a.lph - 1), group = lane / a.lph, per_wave = 64 / a.lph;
     const int D = a.D, half = a.rot / 2;
     const bool holds = l * 8 < D;
     const bool turns = l * 8 < a.rot;
     const int o0 = turns && !PAIRS ? 4 * l : 8 * l, o1 = turns && !PAIRS ? half + 4 * l : 8 * l + 4;
-    float c[4], s[4];
-    const int pos = a.positions[t];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        c[i] = 1.f;
-        s[i] = 0.f;
-        if (turns) {
-            const double n = (double)pos * (a.inv_freq[4 * l + i] * 0.15915494309189533577);
-            sincospif(2.0f * (float)(n - rint(n)), &s[i], &c[i]);
-        }
-    }
+    const int heads = a.n_q + 2 * a.n_kv;
+    const In* const row = (const In*)a.qkv + (int64_t)t * a.row_elements;
     const int64_t slot = a.slots[t];
+    const int pos = a.positions[t];
+    f32x4 c{1.f, 1.f, 1.f, 1.f}, s{0.f, 0.f, 0.f, 0.f};
+    bool angles = false;
     const bool keeps = slot >= 0 && slot < a.pool_tokens;
-    if (slot != -1 && !keeps && a.status && threadIdx.x == 0) atomicOr(a.status, 1);
-    const int64_t page = keeps ? slot / a.P : 0;
+    if (slot != -1 && !keeps && a.status && wave == 0 && lane == 0) atomicOr(a.status, 1);
+    const int64_t page = keeps ? divide((int)slot, a.page_magic, a.page_shift) : 0;
     const int place = keeps ? (int)(slot - page * a.P) : 0;
 
-    const int heads = a.n_q + 2 * a.n_kv;
-    for (int h0 = wave * per_wave; h0 < heads; h0 += kRopeWaves * per_wave) {      // the same number of rounds for all lanes of a wavefront
-        const int h = h0 + group;
-        const bool live = holds && h < heads;
-        float4 x{0.f, 0.f, 0.f, 0.f}, y{0.f, 0.f, 0.f, 0.f};
-        if (live) {
-            const In* src = (const In*)a.qkv + (int64_t)t * a.row_elements + (int64_t)h * D;
-            x = load4(src + o0);
-            y = load4(src + o1);
-        }
-        const bool is_v = h >= a.n_q + a.n_kv;
-        const float* gamma = h < a.n_q ? a.q_gamma : a.k_gamma;
-        float sum = x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w + y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w;
-        for (int m = 1; m < a.lph; m <<= 1) sum += __shfl_xor(sum, m, 64);
-        if (!live) continue;
-        if (!is_v) {
-            if (gamma) {
-                const float r = 1.0f / sqrtf(sum / (float)D + a.eps);
-                const float4 g0 = load4(gamma + o0), g1 = load4(gamma + o1);
-                x = float4{x.x * r * g0.x, x.y * r * g0.y, x.z * r * g0.z, x.w * r * g0.w};
-                y = float4{y.x * r * g1.x, y.y * r * g1.y, y.z * r * g1.z, y.w * r * g1.w};
+    for (int h0 = wave * per_wave; h0 < heads; h0 += AT_ONCE * WAVES * per_wave) {      // the same number of rounds for all lanes of a wavefront
+        f32x4 x[AT_ONCE], y[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int h = h0 + j * WAVES * per_wave + group;
+            x[j] = y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (holds && h < heads) {
+                x[j] = load4<FAR>(row + (int64_t)h * D + o0);
+                y[j] = load4<FAR>(row + (int64_t)h * D + o1);
             }
-            if (turns) {
-                if (PAIRS) {
-                    const float4 u = x, v = y;
-                    x = float4{u.x * c[0] - u.y * s[0], u.y * c[0] + u.x * s[0], u.z * c[1] - u.w * s[1], u.w * c[1] + u.z * s[1]};
-                    y = float4{v.x * c[2] - v.y * s[2], v.y * c[2] + v.x * s[2], v.z * c[3] - v.w * s[3], v.w * c[3] + v.z * s[3]};
-                } else {
-                    const float4 u = x, v = y;
-                    x = float4{u.x * c[0] - v.x * s[0], u.y * c[1] - v.y * s[1], u.z * c[2] - v.z * s[2], u.w * c[3] - v.w * s[3]};
-                    y = float4{v.x * c[0] + u.x * s[0], v.y * c[1] + u.y * s[1], v.z * c[2] + u.z * s[2], v.w * c[3] + u.w * s[3]};
+        }
+        if (!angles) {                                       // once, while the first loads are under way
+            angles = true;
+            if (turns)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float sine, cosine;
+                    sine_cosine((double)pos * (a.inv_freq[4 * l + i] * 0.15915494309189533577), sine, cosine);
+                    s[i] = sine;
+                    c[i] = cosine;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int hw = h0 + j * WAVES * per_wave;        // the wavefront's first
+            if (hw >= heads) break;
+            const int h = hw + group;
+            const bool is_v = h >= a.n_q + a.n_kv;
+            const float* gamma = h < a.n_q ? a.q_gamma : a.k_gamma;
+            f32x4 u = x[j], v = y[j];
+            if (a.q_gamma || a.k_gamma) {                    // a sum over the lanes of the head
+                const f32x4 uu = u * u, vv = v * v;
+                float sum = ((uu.x + uu.y) + (uu.z + uu.w)) + ((vv.x + vv.y) + (vv.z + vv.w));
+                for (int m = 1; m < a.lph; m <<= 1) sum += __shfl_xor(sum, m, 64);
+                if (gamma && !is_v && holds) {
+                    const float r = rsqrtf(fmaf(sum, a.per_element, a.eps));
+                    u = u * r * load4<false>(gamma + o0);
+                    v = v * r * load4<false>(gamma + o1);
                 }
             }
+            if (!is_v) {
+                const f32x4 f = u, g = v;
+                if (PAIRS) {
+                    u = f32x4{f.x * c.x - f.y * s.x, f.y * c.x + f.x * s.x, f.z * c.y - f.w * s.y, f.w * c.y + f.z * s.y};
+                    v = f32x4{g.x * c.z - g.y * s.z, g.y * c.z + g.x * s.z, g.z * c.w - g.w * s.w, g.w * c.w + g.z * s.w};
+                } else if (turns) {
+                    u = f * c - g * s;
+                    v = g * c + f * s;
+                }
+            }
+            if (!holds || h >= heads) continue;
+            Out* dst;
+            if (h < a.n_q) {
+                dst = (Out*)a.q + ((int64_t)t * a.n_q + h) * D;
+            } else {
+                if (!keeps) continue;
+                const int kv = is_v ? h - a.n_q - a.n_kv : h - a.n_q;
+                dst = (Out*)(is_v ? a.v_cache : a.k_cache) + ((page * a.n_kv + kv) * a.P + place) * D;
+            }
+            store4<FAR>(dst + o0, u);
+            store4<FAR>(dst + o1, v);
         }
-        Out* dst;
-        if (h < a.n_q) {
-            dst = (Out*)a.q + ((int64_t)t * a.n_q + h) * D;
-        } else {
-            if (!keeps) continue;
-            const int kv = is_v ? h - a.n_q - a.n_kv : h - a.n_q;
-            dst = (Out*)(is_v ? a.v_cache : a.k_cache) + ((page * a.n_kv + kv) * a.P + place) * D;
-        }
-        store4(dst + o0, x);
-        store4(dst + o1, y);
     }
+}
+
+template <class In, class Out, int WAVES>
+int launch_rope(const RopeArgs& a, bool pairs, hipStream_t st) {
+    constexpr bool far = WAVES == 4;
+    if (pairs) hipLaunchKernelGGL((qk_norm_rope_kernel<In, Out, true, WAVES, far>), dim3(a.T), dim3(WAVES * 64), 0, st, a);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<In, Out, false, WAVES, far>), dim3(a.T), dim3(WAVES * 64), 0, st, a);
+    MOE_HIP_TRY(hipGetLastError());
+    return MOE_OK;
 }
 
 template <class In, class Out>
 int launch_rope(const RopeArgs& a, bool pairs, hipStream_t st) {
-    if (pairs) hipLaunchKernelGGL((qk_norm_rope_kernel<In, Out, true>), dim3(a.T), dim3(kRopeWaves * 64), 0, st, a);
-    else hipLaunchKernelGGL((qk_norm_rope_kernel<In, Out, false>), dim3(a.T), dim3(kRopeWaves * 64), 0, st, a);
-    MOE_HIP_TRY(hipGetLastError());
-    return MOE_OK;
+    return a.T <= kFewRows ? launch_rope<In, Out, 8>(a, pairs, st) : launch_rope<In, Out, 4>(a, pairs, st);
 }
 
 }  // namespace
@@ -380,8 +432,29 @@ int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t 
         return MOE_ERR_INVALID_ARG;
     int lph = 4;
     while (lph * 8 < s->head_dim) lph *= 2;
-    const RopeArgs a{qkv, q_gamma, k_gamma, inv_freq, positions, slots, q, k_cache, v_cache, status, row_elements, s->pool_pages * s->page_tokens, eps,
-                     T, s->n_q, s->n_kv, s->head_dim, s->page_tokens, rot_dim, lph};
+    RopeArgs a{};
+    a.qkv = qkv;
+    a.q_gamma = q_gamma;
+    a.k_gamma = k_gamma;
+    a.inv_freq = inv_freq;
+    a.positions = positions;
+    a.slots = slots;
+    a.q = q;
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    a.status = status;
+    a.row_elements = row_elements;
+    a.pool_tokens = s->pool_pages * s->page_tokens;
+    a.page_magic = division_magic(s->page_tokens, a.page_shift);
+    a.eps = eps;
+    a.per_element = 1.f / (float)s->head_dim;
+    a.T = T;
+    a.n_q = s->n_q;
+    a.n_kv = s->n_kv;
+    a.D = s->head_dim;
+    a.P = s->page_tokens;
+    a.rot = rot_dim;
+    a.lph = lph;
     hipStream_t st = (hipStream_t)stream;
     if (qkv_dtype == MOE_DTYPE_F32)
         return s->dtype == MOE_DTYPE_F32 ? launch_rope<float, float>(a, pairs != 0, st) : launch_rope<float, uint16_t>(a, pairs != 0, st);
