@@ -81,6 +81,10 @@ def main():
                          "(weights resident): --requests seeded prompt lengths (average 77, maximum 418) are packed into "
                          "micro-batches of --ubs requests by paper_2411_11217_amd.batching, and a step runs moe_layer once "
                          "per micro-batch on that micro-batch's prompt tokens")
+    ap.add_argument("--decode", action="store_true",
+                    help="instead of the headline step, time decode steps of --layers attention + MoE layers of --config's shape (one set of "
+                         "weights for all, 32 or 48 query and 8 key/value heads of 128) with the key-value cache in device memory: --ubs requests "
+                         "take their seeded prompts (average 77, maximum 418) in one step, then one token each per step")
     ap.add_argument("--mu-sweep", action="store_true",
                     help="instead of the headline step, time moe_layer on --config's layer shape (weights resident) for "
                          "micro-batch sizes 32 .. 4096: the memory-bound plateau of the decode stage (the paper's section "
@@ -146,6 +150,8 @@ def main():
         return tasks_bench(args, cfg, M, make_inputs)
     if args.prefill:
         return prefill_bench(args, cfg, M, make_inputs)
+    if args.decode:
+        return decode_bench(args, cfg, M, make_inputs)
     if args.mu_sweep:
         return mu_sweep_bench(args, cfg, M, make_inputs)
     if args.splits:
@@ -632,6 +638,59 @@ def prefill_bench(args, cfg, M, make_inputs):
                    "prompt_len_avg": round(float(lens.mean()), 2), "prompt_len_max": int(lens.max()),
                    "micro_batch_tokens": tokens},
         "expert_gemms_tflops_lower_bound": round(flops / (ms * 1e-3) / 1e12, 1)}), flush=True)
+
+
+def decode_bench(args, cfg, M, make_inputs):
+    """Prompts of a micro-batch of requests, then decode steps of one token per request, everything on the GPU."""
+    import torch
+    from moe_workloads import prompt_lengths
+    B, H = args.ubs, cfg.H
+    lens = [int(v) for v in prompt_lengths(B, seed=cfg.seed)]
+    n_kv, D, page_tokens = 8, 128, 16
+    n_q = H // D
+    total_steps = args.warmup + args.steps
+    held = [-(-(n + total_steps) // page_tokens) for n in lens]
+    kv = M.make_kv_shape(n_q, n_kv, D, page_tokens, max(held), sum(held), "bf16")
+    inp = make_inputs(cfg, threads=16)
+    s = M.make_shape(sum(lens), H, cfg.F, cfg.E, cfg.k, cfg.dtype, cfg.page_bytes)
+    pw = M.PagedWeights(s, inp["W1"], inp["W3"], inp["W2"])
+    o_shape, q_shape = M.make_linear_shape(B, H, H, cfg.page_bytes), M.make_linear_shape(B, H, H + 2 * n_kv * D, cfg.page_bytes)
+    n_exp, n_o, n_qkv = pw.pool_pages, M.linear_pages_required(o_shape), M.linear_pages_required(q_shape)
+    g = torch.Generator().manual_seed(1)
+    pool = torch.empty((n_exp + n_o + n_qkv, cfg.page_bytes), dtype=torch.uint8)
+    pool[:n_exp] = pw.pages_host
+    o_table = torch.arange(n_exp, n_exp + n_o, dtype=torch.int32)
+    q_table = torch.arange(n_exp + n_o, n_exp + n_o + n_qkv, dtype=torch.int32)
+    M.linear_pack(o_shape, (torch.randn((o_shape.N, H), generator=g) * 0.02).to(torch.bfloat16), o_table, pool)
+    M.linear_pack(q_shape, (torch.randn((q_shape.N, H), generator=g) * 0.02).to(torch.bfloat16), q_table, pool)
+    ones, head_ones = torch.ones(H).cuda(), torch.ones(D).cuda()
+    layer = M.LayerWeights(pool.cuda(), q_table.cuda(), o_table.cuda(), pw.table_host.cuda(), inp["Wr"].cuda(), ones, ones, None, head_ones, head_ones)
+    inv_freq = torch.tensor([1e6 ** (-2.0 * i / D) for i in range(D // 2)], dtype=torch.float64).cuda()
+    model = M.DecodeLayers(s, kv, [layer] * args.layers, inv_freq, B)
+    prompts = torch.randn((sum(lens), H), generator=g).cuda()
+    tokens = torch.randn((B, H), generator=g).cuda()
+    one_each = torch.ones(B, dtype=torch.int32, device="cuda")
+
+    def timed(n, fn):
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(n):
+            fn()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3 / max(n, 1)
+
+    prompt_ms = timed(1, lambda: model.step(prompts, torch.tensor(lens, dtype=torch.int32, device="cuda")))
+    timed(args.warmup, lambda: model.step(tokens, one_each))
+    ms = timed(args.steps, lambda: model.step(tokens, one_each))
+    if model.status[0].item() != 0 or model.lengths.tolist() != [n + total_steps for n in lens]:
+        raise RuntimeError("decode: a request was refused, status %d" % model.status[0].item())
+    attn_bytes = 4.0 * n_kv * D * (sum(lens) + B * (args.warmup + 0.5 * args.steps))
+    print(json.dumps({
+        "metric": "decode steps of attention + MoE layers with the key-value cache in device memory, tokens/s through all layers", "value": round(B / (ms * 1e-3), 1),
+        "unit": "tokens/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(ms, 4), "ms_per_layer": round(ms / args.layers, 4),
+        "ms_prompts_first_call": round(prompt_ms, 3), "dtype": cfg.dtype, "data": "synthetic",
+        "config": {"workload": cfg.name + " (layer shape), decode", "layers": args.layers, "requests": B, "prompt_tokens": sum(lens), "query_heads": n_q, "kv_heads": n_kv,
+                   "head_dim": D, "page_tokens": page_tokens, "cache_mb_read_per_layer": round(attn_bytes / 1e6, 1)}}), flush=True)
 
 
 def pipeline_bench(args, cfg, M, make_inputs):

@@ -1,0 +1,82 @@
+"""Decode with the key-value cache in device memory: a stack of attention + MoE layers of one shape, stepped over the fresh tokens of a
+batch of requests -- whole prompts, single tokens, or both in one step.
+
+    tables of the step (moe_kv_assign, once)
+    for each layer:  residual + norm + QKV projection (moe_pre_attention), norm and rotation into the layer's cache
+                     (moe_qk_norm_rope), attention over the cache (moe_attn_decode), O projection + residual + norm + MoE layer
+                     (moe_post_attention)
+
+In the paper's decode stage the attention of the middle line runs on the CPU (its section 4.1); here all of a layer is on the GPU.  The
+order of the calls and the buffers between them, nothing else: all arithmetic is the library's.
+"""
+from __future__ import annotations
+
+import dataclasses
+from typing import List, Optional, Sequence, Tuple
+
+import torch
+
+from . import binding as B
+
+
+@dataclasses.dataclass
+class LayerWeights:
+    """One layer's weights in device memory: Wqkv, Wo and the experts in pages of one pool."""
+    page_pool: torch.Tensor              # uint8 [pool_pages, page_bytes]
+    qkv_table: torch.Tensor              # int32 [pages of Wqkv]
+    o_table: torch.Tensor                # int32 [pages of Wo]
+    page_table: torch.Tensor             # int32 [E, pages per expert]
+    Wr: torch.Tensor                     # bf16 [E, H]
+    norm_attn: torch.Tensor              # float32 [H], before the QKV projection
+    norm_moe: torch.Tensor               # float32 [H], before the MoE layer
+    bias: Optional[torch.Tensor] = None
+    q_gamma: Optional[torch.Tensor] = None
+    k_gamma: Optional[torch.Tensor] = None
+
+
+class DecodeLayers:
+    """``shape``: the MoE layer (its T is ignored), ``kv``: heads and cache; ``n_requests`` seats, each with a row of the block
+    table.  The requests' lengths, the pages they hold and the caches of all layers are kept here from step to step."""
+
+    def __init__(self, shape: B.MoEShape, kv: B.KvShape, layers: Sequence[LayerWeights], inv_freq: torch.Tensor, n_requests: int,
+                 eps: float = 1e-5, window: int = 0, device="cuda"):
+        self.shape, self.kv, self.layers, self.n_requests = shape, kv, list(layers), int(n_requests)
+        self.inv_freq, self.eps, self.window = inv_freq, float(eps), int(window)
+        width = (kv.n_q + 2 * kv.n_kv) * kv.head_dim
+        self.qkv_width, self.attn_width = -(-width // 128) * 128, kv.n_q * kv.head_dim
+        self.caches: List[Tuple[torch.Tensor, torch.Tensor]] = [
+            (torch.empty(kv.cache_shape, dtype=kv.torch_dtype, device=device), torch.empty(kv.cache_shape, dtype=kv.torch_dtype, device=device)) for _ in self.layers]
+        self.block_table = torch.full((self.n_requests, kv.max_pages), -1, dtype=torch.int32, device=device)
+        self.free_pages = torch.arange(kv.pool_pages, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(self.n_requests, dtype=torch.int32, device=device)
+        self.free_head = torch.zeros(1, dtype=torch.int32, device=device)
+        self.status = torch.zeros(4, dtype=torch.int32, device=device)
+        self._steps = {}                                  # rows -> two KvSteps and whose turn it is
+        self._workspaces = {}                             # rows -> AttnWorkspace
+
+    def step(self, embedded: torch.Tensor, fresh: torch.Tensor) -> Tuple[torch.Tensor, B.KvStep]:
+        """embedded float32 [T, H]: the fresh tokens of all requests, in the order of the requests; fresh int32 [n_requests].
+        -> (hidden states float32 [T, H] after the last layer, the step's tables).  Nothing waits for the device: a request that does
+        not fit (bits 1 and 2 of status[0]) keeps its length, and its rows of the result mean nothing."""
+        kv, T = self.kv, embedded.shape[0]
+        if T not in self._steps:
+            self._steps[T] = [[B.KvStep(kv, self.n_requests, T, embedded.device) for _ in range(2)], 0]
+            self._workspaces[T] = B.AttnWorkspace(kv, T, embedded.device)
+        pair = self._steps[T]
+        tables = pair[0][pair[1]]
+        pair[1] ^= 1
+        B.moe_kv_assign(kv, self.lengths, fresh, self.free_pages, self.free_head, self.block_table, step=tables, status=self.status)
+        seen = torch.where(tables.slots >= 0, tables.positions + 1, 0)          # rows without a slot attend to nothing
+        s = self.shape.with_tokens(T)
+        qkv_proj = B.make_linear_shape(T, s.H, self.qkv_width, s.page_bytes)
+        o_proj = B.make_linear_shape(T, self.attn_width, s.H, s.page_bytes)
+        hidden, delta = None, embedded
+        for w, (k_cache, v_cache) in zip(self.layers, self.caches):
+            hidden, _, qkv, _ = B.moe_pre_attention(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, want_bf16=False)
+            q = B.moe_qk_norm_rope(kv, qkv, self.inv_freq, tables.positions, tables.slots, k_cache, v_cache, w.q_gamma, w.k_gamma, self.eps, status=self.status)
+            attn, _ = B.moe_attn_decode(kv, q, seen, self.block_table, k_cache, v_cache, window=self.window, table_row=tables.request,
+                                        workspace=self._workspaces[T], status=self.status)
+            hidden, _, delta, _ = B.moe_post_attention(s, o_proj, attn.view(T, self.attn_width), hidden, w.o_table, w.norm_moe, self.eps, w.Wr,
+                                                       w.page_table, w.page_pool, bias=w.bias)
+        self.lengths, self.free_head = tables.seq_len, tables.free_head
+        return hidden + delta, tables
