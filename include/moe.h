@@ -418,7 +418,8 @@ int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t 
  *   q: device dtype[R][n_q][head_dim]; seq_len: device int32[R] (above max_pages * page_tokens: cut there, status bit 0);
  *   block_table: device int32[table_rows][max_pages]; out: device dtype[R][n_q][head_dim]; lse: device float[R][n_q] or NULL,
  *   natural logarithm of the sum of exponentials; workspace: device, 256-byte aligned, moe_attn_workspace_bytes.  Its first
- *   MOE_ATTN_COUNTER_BYTES must be zero before its first use; every call leaves them zero, for any shape and R.
+ *   MOE_ATTN_COUNTER_BYTES must be zero before its first use; every call leaves them zero, for any shape and R.  Two calls
+ *   that overlap in time need two.
  * A row's bits depend on how the rows of its call are split, and so on their lengths; equal calls give equal bits.
  * q, out and the cache 16-byte aligned; R * ceil(max_pages * page_tokens / 16) < 2^31. */
 #define MOE_ATTN_COUNTER_BYTES 16384

@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "moe_internal.h"
+#include "moe_attn_split.h"
 
 using namespace moe;
 
@@ -35,7 +36,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4, kThreads = kWaves * 64;
-constexpr int kLeast = 4, kNear = 4;             // least tiles of a block; how far its ends may move to the end of a row
 
 struct AttnArgs {
     const char *q, *k, *v;
@@ -81,7 +81,7 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, int r, int& flags) {
 // A row without tokens has one tile, in which nothing is seen: its zeros are written like any other result.
 template <int TILE>
 __device__ __forceinline__ int tiles_of(const Row& w) {
-    return max(1, (w.len + TILE - 1) / TILE - w.first / TILE);
+    return max(1, (int)(((uint32_t)w.len + TILE - 1) / TILE) - w.first / TILE);
 }
 
 // Sum over the lanes before this one, and over all of them, by data-parallel moves.
@@ -288,22 +288,20 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             before = __builtin_amdgcn_readfirstlane(s_before[below - 1]);
             for (;; before += in_rows, base += 64) {
                 load_rows(ignored);
-                if (before + in_rows > x) break;
+                if (before + in_rows > x || base + 64 >= a.R) break;
             }
         }
-        at = __ffsll((long long)__ballot(before + ahead + n_rows > x)) - 1;
+        at = max(__ffsll((long long)__ballot(before + ahead + n_rows > x)) - 1, 0);
         start = before + __builtin_amdgcn_readlane(ahead, at);
     };
-    const int share = max((total + a.runs - 1) / a.runs, kLeast);
-    const int near = min(share / 2, kNear);
+    const Runs dealt = deal_tiles(total, a.runs);
     auto bound = [&](int w) __attribute__((always_inline)) {
-        const int x = w * share;
+        const int x = w * dealt.share;
         if (w == 0 || x >= total) return min(x, total);
         find(x);
-        const int end = start + __builtin_amdgcn_readlane(n_rows, at);
-        return x - start <= near ? start : end - x <= near ? end : x;
+        return run_end(dealt, x, start, __builtin_amdgcn_readlane(n_rows, at));
     };
-    if (run * share >= total) return;
+    if (run * dealt.share >= total) return;
     const int b0 = bound(run), b1 = bound(run + 1);
     if (b0 == b1) return;
     const int per_wave = (b1 - b0 + kWaves - 1) / kWaves;
@@ -316,7 +314,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         };
         auto row_now = [&](int x) __attribute__((always_inline)) {
             Now w;
-            w.row = base + at;
+            w.row = min(base + at, a.R - 1);                 // lengths that change during the call spoil its results and nothing else
             w.start = start;
             w.tiles = __builtin_amdgcn_readlane(n_rows, at);
             w.len = __builtin_amdgcn_readlane(rows.len, at);
@@ -430,7 +428,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                     sc[u] = scores(Elem{}, *reinterpret_cast<const u32x4*>(keys + (u * 16 + r) * PITCH + s * 64 + g * 16), qf[s], sc[u]);
             }
             if (more && nxt.row != now.row) load_q(nxt.row);
-            const bool whole = now.t0 >= now.first && now.t0 + TILE <= now.len;
+            const bool whole = now.t0 >= now.first && now.len - now.t0 >= TILE;
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
@@ -562,77 +560,91 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
     if (flags && a.status) atomicOr(a.status, flags);
     __syncthreads();
 
-    // ---- rows that several wavefronts of the block share
-    const int items = ND * 4 * H;                            // (dword d, lane c = g * H + r) of a result
-    auto write_item = [&](int item, int row, const f32x4 (&v)[EPD]) __attribute__((always_inline)) {
-        const int d = item / (4 * H), c = item - d * 4 * H, gg = c / H, rr = c - gg * H;
-        char* out = a.out + ((int64_t)row * a.n_q + head0 + rr) * ROW_BYTES;
+    // ---- rows that several wavefronts of the block share.  Lane (r, g) of a wavefront has the values that it had in the loop, every
+    // kWaves-th dword of them; the parts of a row are read together (one loop over items, parts after parts, took 3 us of a
+    // call of 36 requests).
+    auto write_dword = [&](int row, int head, int group, int d, const f32x4 (&v)[EPD]) __attribute__((always_inline)) {
+        char* out = a.out + ((int64_t)row * a.n_q + head0 + head) * ROW_BYTES;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(out + dword_at<ND>(gg * 4 + i, d)) = pack(Elem{}, v[0][i], v[EPD - 1][i]);
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(out + dword_at<ND>(group * 4 + i, d)) = pack(Elem{}, v[0][i], v[EPD - 1][i]);
     };
     const size_t part_room = far_floats(D, min(a.group, 16));
     float* const my_parts = a.parts + ((size_t)hx * a.runs + run) * 2 * part_room;
-    for (int i0 = 0; i0 < kWaves * 2;) {
-        if (s_split[i0].row < 0) {
-            ++i0;
-            continue;
-        }
-        const Split first = s_split[i0];
-        int i1 = i0 + 1, ends = first.ends;                  // parts i0 .. i1 - 1 are this row's, but for the empty ones
-        for (; i1 < kWaves * 2 && (s_split[i1].row < 0 || s_split[i1].row == first.row); ++i1)
-            if (s_split[i1].row >= 0) ends = s_split[i1].ends;
+    constexpr int PARTS = kWaves * 2;
+    int part_row[PARTS];
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) part_row[k] = __builtin_amdgcn_readfirstlane(s_split[k].row);
+#pragma unroll
+    for (int i0 = 0; i0 < PARTS; ++i0) {
+        if (part_row[i0] < 0) continue;
+        bool before = false;                                 // the row's first part is not this one
+#pragma unroll
+        for (int k = 0; k < i0; ++k) before = before || part_row[k] == part_row[i0];
+        if (before) continue;
+        const int row = part_row[i0];
         const bool begins = i0 & 1;
+        bool ends = false;
+        float top = -INFINITY, m_part[PARTS], l_part[PARTS];
+#pragma unroll
+        for (int k = i0; k < PARTS; ++k) {
+            m_part[k] = -INFINITY;
+            l_part[k] = 0.f;
+            if (part_row[k] != row) continue;
+            m_part[k] = slot_of(k)[H * D + min(r, H - 1)];
+            l_part[k] = slot_of(k)[H * D + H + min(r, H - 1)];
+            ends = s_split[k].ends;                          // the last one says
+        }
+        ends = __builtin_amdgcn_readfirstlane(ends);
+#pragma unroll
+        for (int k = i0; k < PARTS; ++k) top = fmaxf(top, m_part[k]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int k = i0; k < PARTS; ++k) {
+            m_part[k] = __builtin_amdgcn_exp2f(m_part[k] - ref);
+            sum += m_part[k] * l_part[k];
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float log2_sum = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
         float* const global = my_parts + (begins ? part_room : 0);
-        for (int item = threadIdx.x; item < items; item += kThreads) {
-            const int d = item / (4 * H), c = item - d * 4 * H, rr = c % H;
-            float top = -INFINITY, sum = 0.f;
-            for (int k = i0; k < i1; ++k)
-                if (s_split[k].row >= 0) top = fmaxf(top, slot_of(k)[H * D + rr]);
-            const float ref = top == -INFINITY ? 0.f : top;
+        for (int d = wave; d < ND; d += kWaves) {
             f32x4 v[EPD];
 #pragma unroll
             for (int j = 0; j < EPD; ++j) v[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k = i0; k < i1; ++k) {
-                if (s_split[k].row < 0) continue;
-                const float* part = slot_of(k);
-                const float w = __builtin_amdgcn_exp2f(part[H * D + rr] - ref);
-                sum += w * part[H * D + H + rr];
 #pragma unroll
-                for (int j = 0; j < EPD; ++j) v[j] += w * reinterpret_cast<const f32x4*>(part)[(d * EPD + j) * 4 * H + c];
+            for (int k = i0; k < PARTS; ++k) {
+                if (part_row[k] != row) continue;
+#pragma unroll
+                for (int j = 0; j < EPD; ++j) v[j] += m_part[k] * reinterpret_cast<const f32x4*>(slot_of(k))[(d * EPD + j) * 4 * H + g * H + min(r, H - 1)];
             }
+#pragma unroll
+            for (int j = 0; j < EPD; ++j) v[j] *= inv;
+            if (r >= H) continue;
             if (begins && ends) {
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-                for (int j = 0; j < EPD; ++j) v[j] *= inv;
-                write_item(item, first.row, v);
-                if (a.lse && item < H) a.lse[(int64_t)first.row * a.n_q + head0 + rr] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+                write_dword(row, r, g, d, v);
             } else {                                         // divided by its sum, so that one number says what it weighs
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-                for (int j = 0; j < EPD; ++j) put_far(reinterpret_cast<f32x4*>(global) + (d * EPD + j) * 4 * H + c, v[j] * inv);
-                if (item < H) put_far(global + H * D + rr, sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum));
+                for (int j = 0; j < EPD; ++j) put_far(reinterpret_cast<f32x4*>(global) + (d * EPD + j) * 4 * H + g * H + r, v[j]);
             }
         }
-        if (!(begins && ends) && threadIdx.x == 0) s_shared[begins ? 1 : 0] = first;
-        i0 = i1;
+        if (wave == 0 && g == 0 && r < H) {
+            if (!(begins && ends)) put_far(global + H * D + r, log2_sum);
+            else if (a.lse) a.lse[(int64_t)row * a.n_q + head0 + r] = log2_sum * 0.69314718055994530942f;
+        }
+        if (!(begins && ends) && threadIdx.x == 0) s_shared[begins ? 1 : 0] = s_split[i0];
     }
 
     // ---- rows that several blocks share: the one that comes last joins them
     far_stores_done();
     __syncthreads();
     if (s_shared[0].row < 0 && s_shared[1].row < 0) return;
-    // The blocks that a row is split over: one more than there are ends of blocks inside it, which bound() leaves where they are.
-    auto runs_of = [&](const Split& w, int& run0) __attribute__((always_inline)) {
-        run0 = (w.start + near) / share;
-        return (w.start + w.tiles - near - 1) / share - run0 + 1;
-    };
     int32_t* const counters = a.counters + (size_t)hx * a.runs;
     if (threadIdx.x < 2) {
         const Split w = s_shared[threadIdx.x];
         int last = 0;
         if (w.row >= 0) {
             int run0;
-            const int n = runs_of(w, run0);
+            const int n = runs_of_row(dealt, w.start, w.tiles, run0);
             last = atomicAdd(counters + run0, 1) == n - 1;
         }
         s_last[threadIdx.x] = last;
@@ -642,7 +654,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         if (!s_last[which]) continue;
         const Split w = s_shared[which];
         int run0;
-        const int n = runs_of(w, run0);
+        const int n = runs_of_row(dealt, w.start, w.tiles, run0);
         const float* const chain = a.parts + ((size_t)hx * a.runs + run0) * 2 * part_room;     // part k: the second slot of run0, the first of the others
         auto part_of = [&](int k) __attribute__((always_inline)) { return chain + (k ? (size_t)k * 2 : 1) * part_room; };
         // A thread has four values of every part, or of every second, third, .. where there are threads enough; many are loaded at a
@@ -686,8 +698,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             weigh[i * 2 + 1] = sum;
         }
         __syncthreads();
-        for (int item = threadIdx.x; item < items; item += kThreads) {
-            const int d = item / (4 * H), c = item - d * 4 * H;
+        for (int item = threadIdx.x; item < ND * 4 * H; item += kThreads) {
+            const int d = item / (4 * H), c = item - d * 4 * H, group = c / H;      // dword d of lane (c % H, c / H)
             f32x4 v[EPD];
             float top = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -705,7 +717,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 }
                 v[j] *= sum == 0.f ? 0.f : 1.f / sum;
             }
-            write_item(item, w.row, v);
+            write_dword(w.row, c - group * H, group, d, v);
             if (a.lse && item < H) a.lse[(int64_t)w.row * a.n_q + head0 + item] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
         }
         if (threadIdx.x == 0) counters[run0] = 0;            // for the next call: nobody else of this one looks at it again
@@ -727,7 +739,7 @@ Plan plan_of(const moe_kv_shape& s, int32_t R) {
     // Two for each of the 256 compute units, all of them at once.  us with one, two, four: 256 requests 365 / 347 / 377, 36 requests 20 / 20 /
     // 24, one request of 131001 tokens 102 / 102 / 126, 900 prompt rows 69 / 49 / 58.
     constexpr int kBlocks = 512;
-    p.runs = (int)std::max<int64_t>(1, std::min<int64_t>({kBlocks / heads_x, (tiles + kLeast - 1) / kLeast}));
+    p.runs = (int)std::max<int64_t>(1, std::min<int64_t>({kBlocks / heads_x, (tiles + kLeastTiles - 1) / kLeastTiles}));
     p.parts_bytes = (size_t)heads_x * p.runs * 2 * far_floats(s.head_dim, H) * 4;
     p.lds_bytes = (size_t)std::max(kWaves * wave_floats(s.head_dim, H, s.dtype == MOE_DTYPE_BF16 ? 2 : 4), join_floats(s.head_dim, H)) * 4;
     return p;

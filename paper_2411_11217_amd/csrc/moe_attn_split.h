@@ -1,0 +1,42 @@
+// How the tiles of a key/value head's rows are dealt to blocks (moe_attn.hip): integer arithmetic alone, shared by the kernel and a host test.
+#pragma once
+
+#ifndef MOE_HD
+#if defined(__HIPCC__)
+#define MOE_HD __host__ __device__ __forceinline__
+#else
+#define MOE_HD inline
+#endif
+#endif
+
+namespace moe {
+
+// Least tiles of a block: one for each of its wavefronts.  (us with 4 / 8: three short float32 requests 6.4 / 7.3, 36 requests of 60 to 700
+// tokens 16 either way.)
+constexpr int kLeastTiles = 4;
+// How many tiles the end of a block may move to meet the end of a row, so that the row is not shared with another block.  (us
+// with 0 / 2 / 4 / 8: 36 requests of 60 to 700 tokens 19.8 / 17.6 / 16.0 / 16.2, 900 prompt rows 40 / 40 / 37 / 37, long requests the same.)
+constexpr int kNearTiles = 4;
+
+// Block w has the tiles from run_end(w * share) to run_end((w + 1) * share).
+struct Runs {
+    int share, near;
+};
+MOE_HD Runs deal_tiles(int total, int runs) {
+    Runs d;
+    d.share = (total + runs - 1) / runs;
+    if (d.share < kLeastTiles) d.share = kLeastTiles;
+    d.near = d.share / 2 < kNearTiles ? d.share / 2 : kNearTiles;
+    return d;
+}
+// Where the end x of a block, 0 < x < total, in a row with `tiles` tiles from `start` on, is moved.
+MOE_HD int run_end(const Runs& d, int x, int start, int tiles) {
+    return x - start <= d.near ? start : start + tiles - x <= d.near ? start + tiles : x;
+}
+// The blocks run0 .. run0 + n - 1 that a row is split over: one more than there are ends inside it that stay where they are.
+MOE_HD int runs_of_row(const Runs& d, int start, int tiles, int& run0) {
+    run0 = (start + d.near) / d.share;
+    return (start + tiles - d.near - 1) / d.share - run0 + 1;
+}
+
+}  // namespace moe

@@ -140,3 +140,19 @@ def test_oracle_attention_is_a_softmax():
     y, _ = attention.qk_norm_rope(q[:, None], None, 0.0, [0.5, 0.25], [0, 1, 2], True)
     z = (q[:, 0] + 1j * q[:, 1]) * np.exp(0.5j * np.arange(3))
     assert np.allclose(y[:, 0, 0], z.real) and np.allclose(y[:, 0, 1], z.imag) and np.allclose(y[:, 0, 4:], q[:, 4:])
+
+
+def test_tiles_are_dealt_to_blocks_once(tmp_path):
+    """Random rows through the split's arithmetic, and the division by multiplication, under the host sanitizers."""
+    import os
+    import shutil
+    import subprocess
+    if not shutil.which("g++"):
+        pytest.skip("no host compiler")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "attn_split_driver")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-I", os.path.join(root, "include"),
+                        "-I", os.path.join(root, "paper_2411_11217_amd", "csrc"), os.path.join(root, "tests", "attn_split_driver.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "all ok" in r.stdout, (r.stdout[-2000:], r.stderr[-4000:])

@@ -467,6 +467,21 @@ def test_attention_one_workspace_for_calls_of_different_shapes():
         assert (ws.buf[:16384] == 0).all()
 
 
+def test_attention_parts_in_the_workspace_are_never_those_of_a_call_before():
+    # rows that many blocks share, other values call by call, one workspace for all and one of its own for each
+    lens = [5000, 3100]
+    c = Cache(lens, 2, 128, 16, "bf16", 12)
+    kv = M.make_kv_shape(12, 2, 128, 16, c.table.shape[1], c.k.shape[0], "bf16")
+    table, k, seq = c.table.cuda(), c.k.cuda(), i32(lens)
+    ws = M.AttnWorkspace(kv, 2)
+    for i in range(12):
+        v, q = torch.roll(c.v, i, dims=3).cuda(), queries(2, kv, "bf16", i).cuda()
+        out, _ = M.moe_attn_decode(kv, q, seq, table, k, v, workspace=ws)
+        want, _ = M.moe_attn_decode(kv, q, seq, table, k, v)
+        assert torch.equal(out, want) and out.isfinite().all(), i
+    assert (ws.buf[:16384] == 0).all()
+
+
 def test_attention_on_another_stream_and_in_a_graph():
     lens = [3000, 17, 800, 0, 5]
     c = Cache(lens, 2, 128, 16, "bf16", 11)
