@@ -12,8 +12,8 @@ namespace {
 // Two prefix sums over the requests (rows, new pages), then every row, page and request finds its place by itself, with a
 // search in the sums.  One launch: every block forms both sums from the counts (at most 4096 requests, 32 KB that come from
 // the L2) and serves the rows it strides over; a launch for the sums alone would cost more.  A call writes 12 bytes per row; it is bound by
-// the latency of its chain (counts, two sums, page, slot) up to some 100000 rows.  us, in a graph: 36 requests of one token 5.7, 128 prompts
-// of 18600 tokens 7.3, 4000 requests of 529000 rows 15.7.
+// the latency of its chain (counts, two sums, page, slot; 1024 threads, since the sums' part of it grows with the requests per thread) up to some 100000
+// rows.  us in a graph: 36 requests of one token 3.8, 128 prompts of 18600 tokens 6.1, 4000 requests with 529000 rows 16.
 constexpr uint32_t kManyRows = 1u << 30;         // sums stop here: nothing that large is ever served
 constexpr uint32_t kServed = 1u << 31;           // beside a sum of pages
 
@@ -68,8 +68,8 @@ __device__ __forceinline__ int last_at_most(const uint32_t* sums, int n, uint32_
     return lo;
 }
 
-// PER requests to a thread: B <= THREADS * PER.
-template <int THREADS, int PER>
+// PER requests to a thread: B <= THREADS * PER.  ROWS rows to a thread, one search for them.
+template <int THREADS, int PER, int ROWS>
 __global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a) {
     extern __shared__ uint32_t sums[];           // [B] rows before a request, [B] new pages before it and whether it is served
     __shared__ uint32_t row_part[THREADS / 64], page_part[THREADS / 64], s_used;
@@ -143,13 +143,18 @@ __global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a) {
         const int b = last_at_most(page0, a.B, i);
         a.block_table[(size_t)b * a.max_pages + pages_of(a, a.cached[b]) + (int)(i - (page0[b] & ~kServed))] = a.free_pages[head + (int)i];
     }
-    for (uint32_t i = me * 4; i < T; i += step * 4) {        // four rows at a time, one search for them
-        int pos[4] = {0, 0, 0, 0}, slot[4] = {-1, -1, -1, -1}, req[4] = {-1, -1, -1, -1};
+    for (uint32_t i = me * ROWS; i < T; i += step * ROWS) {
+        int pos[ROWS], slot[ROWS], req[ROWS];
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            pos[j] = 0;
+            slot[j] = req[j] = -1;
+        }
         if (i < live) {
             int b = last_at_most(row0, a.B, i), of = -1, last_page = -1, page = -1;
             int had = 0, held = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < ROWS; ++j) {
                 if (i + j >= live) continue;
                 while (b + 1 < a.B && row0[b + 1] <= i + j) ++b;
                 if (b != of) {
@@ -172,13 +177,13 @@ __global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a) {
                 }
             }
         }
-        if (a.vectors && i + 4 <= T) {
-            *reinterpret_cast<int4*>(a.positions + i) = int4{pos[0], pos[1], pos[2], pos[3]};
-            *reinterpret_cast<int4*>(a.slots + i) = int4{slot[0], slot[1], slot[2], slot[3]};
-            *reinterpret_cast<int4*>(a.request + i) = int4{req[0], req[1], req[2], req[3]};
+        if (ROWS == 4 && a.vectors && i + 4 <= T) {
+            *reinterpret_cast<int4*>(a.positions + i) = int4{pos[0], pos[1 % ROWS], pos[2 % ROWS], pos[3 % ROWS]};
+            *reinterpret_cast<int4*>(a.slots + i) = int4{slot[0], slot[1 % ROWS], slot[2 % ROWS], slot[3 % ROWS]};
+            *reinterpret_cast<int4*>(a.request + i) = int4{req[0], req[1 % ROWS], req[2 % ROWS], req[3 % ROWS]};
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < ROWS; ++j)
                 if (i + j < T) {
                     a.positions[i + j] = pos[j];
                     a.slots[i + j] = slot[j];
@@ -189,13 +194,22 @@ __global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a) {
     if (a.status && flags) atomicOr(a.status, flags);
 }
 
-template <int THREADS, int PER>
+template <int THREADS, int PER, int ROWS>
 int launch_assign(const AssignArgs& a, hipStream_t st) {
-    // a block for as many rows (four to a thread) as it has threads; beyond two blocks per compute unit they stride
-    const int blocks = (int)std::min<int64_t>(std::max<int64_t>(((int64_t)a.T + 4 * THREADS - 1) / (4 * THREADS), 1), 2 * 256 * 256 / THREADS);
-    hipLaunchKernelGGL((assign_kernel<THREADS, PER>), dim3(blocks), dim3(THREADS), (size_t)a.B * 8, st, a);
+    // a block for as many rows as its threads take at once; beyond two blocks of 256 threads per compute unit they stride
+    const int blocks = (int)std::min<int64_t>(std::max<int64_t>(((int64_t)a.T + ROWS * THREADS - 1) / (ROWS * THREADS), 1), 2 * 256 * 256 / THREADS);
+    hipLaunchKernelGGL((assign_kernel<THREADS, PER, ROWS>), dim3(blocks), dim3(THREADS), (size_t)a.B * 8, st, a);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
+}
+
+// Four rows to a thread save searches and stores where there are many; the rows of single tokens are as many requests, and then
+// each is a chain of loads of its own.  us in a graph, one row / four: 36 single tokens 3.7 / 5.7, 4000 9.7 / 11.9, 60000 rows of 250 prompts 6.1 / 7.6, 73000 of
+// 500 8.5 / 9.9, 150000 of 256 7.4 / 7.5, 200000 of 2000 11.5 / 11.3, 529000 of 4000 19.2 / 16.8.
+constexpr int kSingleRows = 1 << 17;
+template <int THREADS, int PER>
+int launch_assign(const AssignArgs& a, hipStream_t st) {
+    return a.T <= kSingleRows ? launch_assign<THREADS, PER, 1>(a, st) : launch_assign<THREADS, PER, 4>(a, st);
 }
 
 // ---- norm and rotation of queries and keys, the write into the cache --------------------------
