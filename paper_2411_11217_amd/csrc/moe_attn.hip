@@ -13,14 +13,19 @@
 // tiles, so which block that is changes no bit).
 //   Where a run starts is found by every block itself, from the lengths on the device: a prefix sum over all rows.
 //
-// Registers instead of LDS.  Keys are the A operand of an MFMA (16 tokens), the up to 16 query heads of the key/value head the
-// B operand: lane (r, g) = (lane % 16, lane / 16) loads 16 bytes of token r's row, and gets back the scores of tokens
-// 4 g .. 4 g + 3 against head r.  For the second product the lane needs values of exactly these tokens, as A operand one
-// element d per MFMA: it loads d-chunk r of each of its four tokens, whole rows per instruction, and the transposition
-// into pairs of tokens stays inside the lane (v_perm).  So the weights never leave the lane that computed them, maxima
-// cross the four lane groups and nothing else does, and LDS is not used in the loop.
+// Products.  Keys are the A operand of an MFMA (16 tokens), the up to 16 query heads of the key/value head the B operand: lane (r, g) =
+// (lane % 16, lane / 16) has 16 bytes of token r's row, and gets back the scores of tokens 4 g .. 4 g + 3 against head r.
+// For the second product the lane needs values of exactly these tokens, as A operand one element d per MFMA: it loads
+// d-chunk r of each of its four tokens, whole rows per instruction, and the transposition into pairs of tokens stays
+// inside the lane (v_perm).  So the weights never leave the lane that computed them, and only maxima cross the four lane groups.
 //   bf16: 32 tokens are the 32 steps of one 16x16x32 MFMA.  The weights are split into two bf16 parts, 16 bits of each weight: half
 // a bf16 step on the weights would show in the outputs.  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded.
+//   The matrix cores are busy a quarter of the time (131001 tokens, 48 heads), so the columns that fewer than 16 heads leave empty cost nothing.
+//
+// us in a graph, and what of the bytes that is (a load-only kernel reads 6.2 TB/s here, 7.1 with the non-temporal hint; an empty launch takes 2):
+// three float32 requests of up to 130 tokens 4.8; 36 requests of 60 to 700 tokens, 32 / 8 heads of 128, 15 (2.4 TB/s); 900 rows of six
+// prompts 37 (310 MB of L2 hits); one request of 131001 tokens, 48 / 8 heads, 95 (5.7 TB/s); a window of 1000 tokens over 61
+// requests, 20 / 20 heads of 96, 76 (5.2 TB/s); 256 requests of 500 to 5000 tokens, 32 / 8 heads, 325 (6.3 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -736,8 +741,8 @@ Plan plan_of(const moe_kv_shape& s, int32_t R) {
     p.head_tiles = (group + 15) / 16;
     const int64_t heads_x = (int64_t)s.n_kv * p.head_tiles;
     const int64_t tiles = R * (((int64_t)s.max_pages * s.page_tokens + tile - 1) / tile);
-    // Two for each of the 256 compute units, all of them at once.  us with one, two, four: 256 requests 365 / 347 / 377, 36 requests 20 / 20 /
-    // 24, one request of 131001 tokens 102 / 102 / 126, 900 prompt rows 69 / 49 / 58.
+    // Two for each of the 256 compute units, all of them at once.  us with one, two, four, in an earlier build: 256 requests 365 / 347 / 377,
+    // 36 requests 20 / 20 / 24, one request of 131001 tokens 102 / 102 / 126, 900 prompt rows 69 / 49 / 58.
     constexpr int kBlocks = 512;
     p.runs = (int)std::max<int64_t>(1, std::min<int64_t>({kBlocks / heads_x, (tiles + kLeastTiles - 1) / kLeastTiles}));
     p.parts_bytes = (size_t)heads_x * p.runs * 2 * far_floats(s.head_dim, H) * 4;
