@@ -24,7 +24,7 @@
 //
 // us in a graph, and what of the bytes that is (a load-only kernel reads 6.2 TB/s here, 7.1 with the non-temporal hint; an empty launch takes 2):
 // three float32 requests of up to 130 tokens 4.8; 36 requests of 60 to 700 tokens, 32 / 8 heads of 128, 15 (2.4 TB/s); 900 rows of six
-// prompts 37 (310 MB of L2 hits); one request of 131001 tokens, 48 / 8 heads, 95 (5.7 TB/s); a window of 1000 tokens over 61
+// prompts 26; one request of 131001 tokens, 48 / 8 heads, 95 (5.7 TB/s); a window of 1000 tokens over 61
 // requests, 20 / 20 heads of 96, 76 (5.2 TB/s); 256 requests of 500 to 5000 tokens, 32 / 8 heads, 325 (6.3 TB/s).
 #include <algorithm>
 #include <type_traits>
@@ -52,7 +52,7 @@ struct AttnArgs {
     int32_t* status;
     uint64_t page_magic;
     int page_shift;
-    int R, n_q, n_kv, group, head_tiles, P, max_pages, table_rows, window, runs;
+    int R, n_q, n_kv, group, head_tiles, pack, P, max_pages, table_rows, window, runs;
     uint32_t pool_pages;
     float scale_log2;
 };
@@ -87,6 +87,21 @@ __device__ __forceinline__ Row row_of(const AttnArgs& a, int r, int& flags) {
 template <int TILE>
 __device__ __forceinline__ int tiles_of(const Row& w) {
     return max(1, (int)(((uint32_t)w.len + TILE - 1) / TILE) - w.first / TILE);
+}
+
+// Rows of prompts.  `pack` rows in a row (16 / heads, from a multiple of `pack` on) that see tokens of one request, up to 8 heads each,
+// share the 16 columns of the MFMA: their tiles are read once instead of once per row.  They do where that is no more tiles than
+// the rows one by one have.  A tile that all of them see whole takes one pass.  In any other the scores are masked column
+// by column, and the second product is made once for each row, with the tokens that this row does not see taken out and the other
+// columns left as they were: a later token's infinity would not be stopped by a weight of 0.
+struct Group {
+    int lo, hi, sum;                             // tokens that some row sees; tiles of the rows one by one
+    bool one;                                    // a full group, tokens everywhere, one request
+};
+template <int TILE>
+__device__ __forceinline__ int joint_tiles(const Group& g) {      // 0: they do not share
+    const int n = (int)(((uint32_t)g.hi + TILE - 1) / TILE) - g.lo / TILE;
+    return g.one && n <= g.sum ? n : 0;
 }
 
 // Sum over the lanes before this one, and over all of them, by data-parallel moves.
@@ -218,10 +233,11 @@ constexpr int join_floats(int D, int H) { return 6 * (kThreads > D * H / 4 ? kTh
 
 struct Split {                                   // a row that a wavefront shares with others
     int row, start, tiles;                       // row -1: none; tiles from `start` on
+    int cols;                                    // its columns that are results
     int ends;                                    // this part has the row's last tile
 };
 
-template <class Elem, int D, bool ONCE>
+template <class Elem, int D, bool ONCE, bool PACKED>
 __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const AttnArgs a) {
     constexpr int TILE = Kind<Elem>::kTile, SUB = TILE / 16, EPD = Kind<Elem>::kPerDword;
     constexpr int ROW_BYTES = D * (int)sizeof(Elem), KS = ROW_BYTES / 64, ND = ROW_BYTES / 64, E = D / 16;
@@ -240,7 +256,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
     const int heads_x = a.n_kv * a.head_tiles;
     const int run = blockIdx.x / heads_x, hx = blockIdx.x - run * heads_x;
     const int kv = hx % a.n_kv, tile0 = hx / a.n_kv * 16;    // key/value head, first of its query heads
-    const int H = min(a.group - tile0, 16);
+    const int H = PACKED ? a.pack * a.group : min(a.group - tile0, 16);      // columns: query heads, of `pack` rows
+    const int col_row = PACKED ? min(r, H - 1) / a.group : 0, col_head = min(r, H - 1) - col_row * a.group;      // of a group that shares them
+    const int window_rows = PACKED ? 64 / a.pack * a.pack : 64;
     const int head0 = kv * a.group + tile0;
     int flags = 0;
     const int part_size = part_floats(D, H), wave_size = wave_floats(D, H, (int)sizeof(Elem));
@@ -251,22 +269,69 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
 
     // ---- which tiles
     int base = 0, start = 0, at = 0;                         // lane i has row base + i; row base + at is the current one, its first tile is `start`
-    Row rows;
-    int n_rows, ahead, in_rows;                              // tiles of the lane's row, of the rows before it, of all 64
+    Row rows, own;                                           // rows: of a group that shares its columns, what some row sees; own: the lane's row
+    int clear_lo, clear_hi;                                  // what all of them see
+    int joint;
+    int n_rows, ahead, in_rows;                              // tiles of the lane's row (of the group: its first lane's), of the rows before it, of all
     auto load_rows = [&](int& report) __attribute__((always_inline)) {
         const int i = base + lane;
-        rows = row_of(a, min(i, a.R - 1), report);
-        n_rows = i < a.R ? tiles_of<TILE>(rows) : 0;
+        const bool live = lane < window_rows && i < a.R;
+        own = rows = row_of(a, min(i, a.R - 1), report);
+        n_rows = live ? tiles_of<TILE>(rows) : 0;
+        if constexpr (PACKED) {
+            const int lead = lane - lane % a.pack;
+            const uint64_t fit = __ballot(live && own.len > 0 && own.table == __shfl(own.table, lead, 64)), all = ((1ull << a.pack) - 1) << lead;
+            Group grp{own.first, own.len, 0, live && (fit & all) == all};
+            clear_lo = own.first;
+            clear_hi = own.len;
+            for (int j = 0; j < a.pack; ++j) {
+                const int len = __shfl(own.len, lead + j, 64), first = __shfl(own.first, lead + j, 64);
+                grp.sum += __shfl(n_rows, lead + j, 64);
+                grp.lo = min(grp.lo, first);
+                grp.hi = max(grp.hi, len);
+                clear_lo = max(clear_lo, first);
+                clear_hi = min(clear_hi, len);
+            }
+            const int shared = joint_tiles<TILE>(grp);
+            joint = shared > 0;
+            if (joint) {
+                n_rows = lane == lead ? shared : 0;
+                rows.first = grp.lo;
+                rows.len = grp.hi;
+            } else {
+                clear_lo = own.first;
+                clear_hi = own.len;
+            }
+        }
         ahead = wave_sum_before(n_rows, in_rows);
     };
+    auto tiles_from = [&](int i) __attribute__((always_inline)) {      // of row i, or of the `pack` rows from i on
+        if constexpr (!PACKED) {
+            return tiles_of<TILE>(row_of(a, i, flags));
+        } else {
+            Group grp{0x7fffffff, 0, 0, i + a.pack <= a.R};
+            int table = 0;
+            for (int j = 0; j < a.pack && i + j < a.R; ++j) {
+                const Row w = row_of(a, i + j, flags);
+                if (j == 0) table = w.table;
+                grp.one = grp.one && w.len > 0 && w.table == table;
+                grp.lo = min(grp.lo, w.first);
+                grp.hi = max(grp.hi, w.len);
+                grp.sum += tiles_of<TILE>(w);
+            }
+            const int shared = joint_tiles<TILE>(grp);
+            return shared > 0 ? shared : grp.sum;
+        }
+    };
     int ignored = 0, total, per = 0;
-    if (a.R <= 64) {                                         // every wavefront has them all
+    if (a.R <= window_rows) {                                // every wavefront has them all
         load_rows(flags);
         total = in_rows;
     } else {
         per = (a.R + kThreads - 1) / kThreads;
+        if (PACKED) per = (per + a.pack - 1) / a.pack * a.pack;
         int mine = 0;
-        for (int i = threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, a.R); ++i) mine += tiles_of<TILE>(row_of(a, i, flags));
+        for (int i = threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, a.R); i += PACKED ? a.pack : 1) mine += tiles_from(i);
         int sum, before = wave_sum_before(mine, sum);
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
@@ -291,9 +356,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             for (int j = 0; j < kWaves; ++j) below += __popcll(__ballot(s_before[j * 64 + lane] <= x));
             base = (below - 1) * per;
             before = __builtin_amdgcn_readfirstlane(s_before[below - 1]);
-            for (;; before += in_rows, base += 64) {
+            for (;; before += in_rows, base += window_rows) {
                 load_rows(ignored);
-                if (before + in_rows > x || base + 64 >= a.R) break;
+                if (before + in_rows > x || base + window_rows >= a.R) break;
             }
         }
         at = max(__ffsll((long long)__ballot(before + ahead + n_rows > x)) - 1, 0);
@@ -316,6 +381,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         find(x0);
         struct Now {                                         // a row and a tile in it, the same for the whole wavefront
             int row, start, tiles, len, first, table, t0;    // t0: first token of the tile
+            int clear_lo, clear_hi, cols;                    // the rest is PACKED's; of the columns cols are results
+            int col_first, col_len;                          // what the lane's column sees
         };
         auto row_now = [&](int x) __attribute__((always_inline)) {
             Now w;
@@ -326,6 +393,17 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             w.first = __builtin_amdgcn_readlane(rows.first, at);
             w.table = __builtin_amdgcn_readlane(rows.table, at);
             w.t0 = (w.first / TILE + x - start) * TILE;
+            w.clear_lo = w.first;
+            w.clear_hi = w.len;
+            w.cols = H;
+            if constexpr (PACKED) {
+                const bool all = __builtin_amdgcn_readlane(joint, at) != 0;
+                w.clear_lo = __builtin_amdgcn_readlane(clear_lo, at);
+                w.clear_hi = __builtin_amdgcn_readlane(clear_hi, at);
+                w.cols = all ? H : a.group;
+                w.col_first = __shfl(own.first, at + (all ? col_row : 0), 64);
+                w.col_len = __shfl(own.len, at + (all ? col_row : 0), 64);
+            }
             return w;
         };
         auto next_of = [&](const Now& w, int x) __attribute__((always_inline)) {      // tile x, the one behind w's
@@ -335,11 +413,13 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 return n;
             }
             start = w.start + w.tiles;
-            if (++at == 64) {
-                base += 64;
-                at = 0;
-                load_rows(ignored);
-            }
+            do {                                             // the next row, or group, that has tiles
+                if (++at == window_rows) {
+                    base += window_rows;
+                    at = 0;
+                    load_rows(ignored);
+                }
+            } while (PACKED && base < a.R && __builtin_amdgcn_readlane(n_rows, at) == 0);
             return row_now(x);
         };
         uint32_t* const places = reinterpret_cast<uint32_t*>(s_parts + (wave + 1) * wave_size) - TILE;
@@ -398,8 +478,10 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 load_tile(a.v, vr);
             }
         };
-        auto load_q = [&](int row) __attribute__((always_inline)) {
-            const char* p = a.q + ((int64_t)row * a.n_q + head0 + min(r, H - 1)) * ROW_BYTES + g * 16;
+        auto load_q = [&](const Now& w) __attribute__((always_inline)) {
+            const bool all = PACKED && w.cols > a.group;
+            const int row = w.row + (all ? col_row : 0), head = PACKED ? (all ? col_head : min(r, a.group - 1)) : min(r, H - 1);
+            const char* p = a.q + ((int64_t)row * a.n_q + head0 + head) * ROW_BYTES + g * 16;
 #pragma unroll
             for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const u32x4*>(p + s * 64);
         };
@@ -412,7 +494,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         Now now = row_now(x0);
         int from = x0;                                       // the first tile of the current row that is this wavefront's
         place(now);
-        load_q(now.row);
+        load_q(now);
         load_tile(a.k, kr);
         load_v();
         Now nxt = now;
@@ -432,8 +514,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 for (int s = 0; s < KS; ++s)
                     sc[u] = scores(Elem{}, *reinterpret_cast<const u32x4*>(keys + (u * 16 + r) * PITCH + s * 64 + g * 16), qf[s], sc[u]);
             }
-            if (more && nxt.row != now.row) load_q(nxt.row);
-            const bool whole = now.t0 >= now.first && now.len - now.t0 >= TILE;
+            if (more && nxt.row != now.row) load_q(nxt);
+            const bool whole = now.t0 >= now.clear_lo && now.clear_hi - now.t0 >= TILE;
+            const int see_from = PACKED ? now.col_first : now.first, see_to = PACKED ? now.col_len : now.len;
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
@@ -445,7 +528,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int t = now.t0 + u * 16 + g * 4 + i;
-                        if (t < now.first || t >= now.len) sc[u][i] = -INFINITY;
+                        if (t < see_from || t >= see_to) sc[u][i] = -INFINITY;
                     }
             }
 #pragma unroll
@@ -475,44 +558,66 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
 #pragma unroll
                     for (int i = 0; i < 4; ++i) load_row<ND, false>(keys + (u * 16 + g * 4 + i) * PITCH, r, vf[u][i]);
             }
-            if (!whole) {                                    // weight 0 times whatever the repeated token holds is not always 0
+            // Adds the tile's weighted values, of the tokens from `from_t` to `to_t` if not of all, to the columns that are `mine`: weight 0 times
+            // whatever a repeated or later token holds is not always 0.
+            auto add_values = [&](bool all, int from_t, int to_t, auto some_c, bool mine) __attribute__((always_inline)) {
+                constexpr bool some = decltype(some_c)::value;
+                uint32_t v[SUB][4][ND];
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = now.t0 + u * 16 + g * 4 + i;
-                        const bool seen = t >= now.first && t < now.len;
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) vf[u][i][d] = seen ? vf[u][i][d] : 0;
-                    }
-            }
-            if constexpr (SUB == 2) {
-                u32x4 hi, lo;
+                        for (int d = 0; d < ND; ++d) v[u][i][d] = vf[u][i][d];
+                if (!all) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        const uint32_t p0 = __float_as_uint(sc[u][i]), p1 = __float_as_uint(sc[u][i + 1]);
-                        hi[u * 2 + i / 2] = high_halves(p0, p1);
-                        const float r0 = sc[u][i] - __uint_as_float(p0 & 0xffff0000u), r1 = sc[u][i + 1] - __uint_as_float(p1 & 0xffff0000u);
-                        lo[u * 2 + i / 2] = high_halves(__float_as_uint(r0), __float_as_uint(r1));
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            const int t = now.t0 + u * 16 + g * 4 + i;
+                            const bool seen = t >= from_t && t < to_t;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const u32x4 even = {low_halves(vf[0][0][d], vf[0][1][d]), low_halves(vf[0][2][d], vf[0][3][d]),
-                                        low_halves(vf[1][0][d], vf[1][1][d]), low_halves(vf[1][2][d], vf[1][3][d])};
-                    const u32x4 odd = {high_halves(vf[0][0][d], vf[0][1][d]), high_halves(vf[0][2][d], vf[0][3][d]),
-                                       high_halves(vf[1][0][d], vf[1][1][d]), high_halves(vf[1][2][d], vf[1][3][d])};
-                    acc[d * 2] = scores(uint16_t{}, even, hi, acc[d * 2]);
-                    acc[d * 2 + 1] = scores(uint16_t{}, odd, hi, acc[d * 2 + 1]);
-                    acc[d * 2] = scores(uint16_t{}, even, lo, acc[d * 2]);
-                    acc[d * 2 + 1] = scores(uint16_t{}, odd, lo, acc[d * 2 + 1]);
+                            for (int d = 0; d < ND; ++d) v[u][i][d] = seen ? v[u][i][d] : 0;
+                        }
                 }
+                if constexpr (SUB == 2) {
+                    u32x4 hi, lo;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const uint32_t p0 = __float_as_uint(sc[u][i]), p1 = __float_as_uint(sc[u][i + 1]);
+                            hi[u * 2 + i / 2] = high_halves(p0, p1);
+                            const float r0 = sc[u][i] - __uint_as_float(p0 & 0xffff0000u), r1 = sc[u][i + 1] - __uint_as_float(p1 & 0xffff0000u);
+                            lo[u * 2 + i / 2] = high_halves(__float_as_uint(r0), __float_as_uint(r1));
+                        }
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const u32x4 even = {low_halves(v[0][0][d], v[0][1][d]), low_halves(v[0][2][d], v[0][3][d]),
+                                            low_halves(v[1][0][d], v[1][1][d]), low_halves(v[1][2][d], v[1][3][d])};
+                        const u32x4 odd = {high_halves(v[0][0][d], v[0][1][d]), high_halves(v[0][2][d], v[0][3][d]),
+                                           high_halves(v[1][0][d], v[1][1][d]), high_halves(v[1][2][d], v[1][3][d])};
+                        f32x4 x = scores(uint16_t{}, even, hi, acc[d * 2]), y = scores(uint16_t{}, odd, hi, acc[d * 2 + 1]);
+                        x = scores(uint16_t{}, even, lo, x);
+                        y = scores(uint16_t{}, odd, lo, y);
+                        acc[d * 2] = !some || mine ? x : acc[d * 2];
+                        acc[d * 2 + 1] = !some || mine ? y : acc[d * 2 + 1];
+                    }
+                } else {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        f32x4 x = acc[d];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][i][d]), sc[0][i], x, 0, 0, 0);
+                        acc[d] = !some || mine ? x : acc[d];
+                    }
+                }
+            };
+            if (PACKED && !whole && now.cols > a.group) {
+                for (int j = 0; j < a.pack; ++j)
+                    add_values(false, __builtin_amdgcn_readlane(now.col_first, j * a.group), __builtin_amdgcn_readlane(now.col_len, j * a.group), std::true_type{}, col_row == j);
             } else {
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[0][i][d]), sc[0][i], acc[d], 0, 0, 0);
+                add_values(whole, now.first, now.len, std::false_type{}, true);
             }
             if (more) load_v();
             const bool ends = x + 1 == now.start + now.tiles;
@@ -521,8 +626,10 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 const bool begins = from == now.start;
                 if (begins && ends) {
                     const float inv = l == 0.f ? 0.f : 1.f / l;
-                    if (r < H) {
-                        char* out = a.out + ((int64_t)now.row * a.n_q + head0 + r) * ROW_BYTES;
+                    if (r < now.cols) {
+                        const bool all = PACKED && now.cols > a.group;
+                        const int64_t at_row = (int64_t)(now.row + (all ? col_row : 0)) * a.n_q + head0 + (all ? col_head : r);
+                        char* out = a.out + at_row * ROW_BYTES;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             uint32_t v[ND];
@@ -530,7 +637,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                             for (int d = 0; d < ND; ++d) v[d] = pack(Elem{}, acc[d * EPD][i] * inv, acc[d * EPD + EPD - 1][i] * inv);
                             store_row<ND>(out, g * 4 + i, v);
                         }
-                        if (a.lse && g == 0) a.lse[(int64_t)now.row * a.n_q + head0 + r] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+                        if (a.lse && g == 0) a.lse[at_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
                     }
                 } else {
                     const int slot = wave * 2 + (begins ? 1 : 0);
@@ -543,7 +650,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                             part[H * D + H + r] = l;
                         }
                     }
-                    if (lane == 0) s_split[slot] = Split{now.row, now.start, now.tiles, ends ? 1 : 0};
+                    if (lane == 0) s_split[slot] = Split{now.row, now.start, now.tiles, now.cols, ends ? 1 : 0};
                 }
                 m = -INFINITY;
                 l = 0.f;
@@ -568,12 +675,16 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
     // ---- rows that several wavefronts of the block share.  Lane (r, g) of a wavefront has the values that it had in the loop, every
     // kWaves-th dword of them; the parts of a row are read together (one loop over items, parts after parts, took 3 us of a
     // call of 36 requests).
-    auto write_dword = [&](int row, int head, int group, int d, const f32x4 (&v)[EPD]) __attribute__((always_inline)) {
-        char* out = a.out + ((int64_t)row * a.n_q + head0 + head) * ROW_BYTES;
+    auto place_of = [&](int row, int col) __attribute__((always_inline)) {      // of a column's result, among all heads of all rows
+        const int further = PACKED ? col / a.group : 0;
+        return (int64_t)(row + further) * a.n_q + head0 + col - further * a.group;
+    };
+    auto write_dword = [&](int row, int col, int group, int d, const f32x4 (&v)[EPD]) __attribute__((always_inline)) {
+        char* out = a.out + place_of(row, col) * ROW_BYTES;
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(out + dword_at<ND>(group * 4 + i, d)) = pack(Elem{}, v[0][i], v[EPD - 1][i]);
     };
-    const size_t part_room = far_floats(D, min(a.group, 16));
+    const size_t part_room = far_floats(D, PACKED ? H : min(a.group, 16));
     float* const my_parts = a.parts + ((size_t)hx * a.runs + run) * 2 * part_room;
     constexpr int PARTS = kWaves * 2;
     int part_row[PARTS];
@@ -586,7 +697,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
 #pragma unroll
         for (int k = 0; k < i0; ++k) before = before || part_row[k] == part_row[i0];
         if (before) continue;
-        const int row = part_row[i0];
+        const int row = part_row[i0], cols = s_split[i0].cols;
         const bool begins = i0 & 1;
         bool ends = false;
         float top = -INFINITY, m_part[PARTS], l_part[PARTS];
@@ -626,7 +737,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             for (int j = 0; j < EPD; ++j) v[j] *= inv;
             if (r >= H) continue;
             if (begins && ends) {
-                write_dword(row, r, g, d, v);
+                if (r < cols) write_dword(row, r, g, d, v);
             } else {                                         // divided by its sum, so that one number says what it weighs
 #pragma unroll
                 for (int j = 0; j < EPD; ++j) put_far(reinterpret_cast<f32x4*>(global) + (d * EPD + j) * 4 * H + g * H + r, v[j]);
@@ -634,7 +745,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         }
         if (wave == 0 && g == 0 && r < H) {
             if (!(begins && ends)) put_far(global + H * D + r, log2_sum);
-            else if (a.lse) a.lse[(int64_t)row * a.n_q + head0 + r] = log2_sum * 0.69314718055994530942f;
+            else if (a.lse && r < cols) a.lse[place_of(row, r)] = log2_sum * 0.69314718055994530942f;
         }
         if (!(begins && ends) && threadIdx.x == 0) s_shared[begins ? 1 : 0] = s_split[i0];
     }
@@ -722,8 +833,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 }
                 v[j] *= sum == 0.f ? 0.f : 1.f / sum;
             }
-            write_dword(w.row, c - group * H, group, d, v);
-            if (a.lse && item < H) a.lse[(int64_t)w.row * a.n_q + head0 + item] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+            if (c - group * H < w.cols) write_dword(w.row, c - group * H, group, d, v);
+            if (a.lse && item < w.cols) a.lse[place_of(w.row, item)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
         }
         if (threadIdx.x == 0) counters[run0] = 0;            // for the next call: nobody else of this one looks at it again
         __syncthreads();
@@ -732,12 +843,14 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
 
 // The launch: `runs` blocks for each key/value head and 16 of its query heads.
 struct Plan {
-    int head_tiles, runs;
+    int head_tiles, runs, pack;
     size_t parts_bytes, lds_bytes;
 };
-Plan plan_of(const moe_kv_shape& s, int32_t R) {
+Plan plan_of(const moe_kv_shape& s, int32_t R, bool prompts) {
     Plan p;
-    const int group = s.n_q / s.n_kv, H = std::min(group, 16), tile = s.dtype == MOE_DTYPE_BF16 ? Kind<uint16_t>::kTile : Kind<float>::kTile;
+    const int group = s.n_q / s.n_kv;
+    p.pack = prompts && group <= 8 ? 16 / group : 1;
+    const int H = std::min(group * p.pack, 16), tile = s.dtype == MOE_DTYPE_BF16 ? Kind<uint16_t>::kTile : Kind<float>::kTile;
     p.head_tiles = (group + 15) / 16;
     const int64_t heads_x = (int64_t)s.n_kv * p.head_tiles;
     const int64_t tiles = R * (((int64_t)s.max_pages * s.page_tokens + tile - 1) / tile);
@@ -757,20 +870,24 @@ int check_rows(const moe_kv_shape* s, int32_t R) {
     return R < 0 || R * tiles > INT32_MAX ? MOE_ERR_INVALID_ARG : MOE_OK;
 }
 
-template <class Elem, int D, bool ONCE>
+template <class Elem, int D, bool ONCE, bool PACKED>
 int launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
-    if (p.lds_bytes > 64 * 1024)
-        MOE_HIP_TRY(hipFuncSetAttribute((const void*)attn_kernel<Elem, D, ONCE>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds_bytes));
-    hipLaunchKernelGGL((attn_kernel<Elem, D, ONCE>), dim3((uint32_t)p.runs * a.n_kv * p.head_tiles), dim3(kThreads), p.lds_bytes, st, a);
+    const auto kernel = attn_kernel<Elem, D, ONCE, PACKED>;
+    if (p.lds_bytes > 64 * 1024) MOE_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds_bytes));
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)p.runs * a.n_kv * p.head_tiles), dim3(kThreads), p.lds_bytes, st, a);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }
 
 // Rows with a table row of their own and at most 16 query heads to a key/value head read every key and value once: those loads carry
-// the non-temporal hint (us without / with: 256 requests 374 / 347, one request of 131001 tokens 114 / 102).
+// the non-temporal hint (us without / with: 256 requests 374 / 347, one request of 131001 tokens 114 / 102).  Rows that name their table row
+// may be a prompt's, and share columns where there is room for two.  us, each row by itself / sharing, 32 / 8 heads of 128: 900 rows of six
+// prompts 37 / 26, 18600 rows of 128 prompts 724 / 347, a prompt of 4000 tokens 1492 / 500, 2200 rows of 200 prompts of 5 to 20 tokens 31 /
+// 32; 20 / 20 heads of 96, three prompts of up to 418 tokens 54 / 36; float32, 8 / 2 heads 28.7 / 28.2.
 template <class Elem, int D>
 int launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
-    return a.table_row || a.head_tiles > 1 ? launch<Elem, D, false>(a, p, st) : launch<Elem, D, true>(a, p, st);
+    if (p.pack > 1) return launch<Elem, D, false, true>(a, p, st);
+    return a.table_row || a.head_tiles > 1 ? launch<Elem, D, false, false>(a, p, st) : launch<Elem, D, true, false>(a, p, st);
 }
 
 template <class Elem>
@@ -795,7 +912,7 @@ int moe_attn_workspace_bytes(const moe_kv_shape* s, int32_t R, size_t* bytes) {
     int rc = check_rows(s, R);
     if (rc != MOE_OK) return rc;
     if (!bytes) return MOE_ERR_INVALID_ARG;
-    *bytes = MOE_ATTN_COUNTER_BYTES + plan_of(*s, R).parts_bytes;
+    *bytes = MOE_ATTN_COUNTER_BYTES + std::max(plan_of(*s, R, false).parts_bytes, plan_of(*s, R, true).parts_bytes);      // with and without table_row
     return MOE_OK;
 }
 
@@ -810,8 +927,10 @@ int moe_attn_decode(const moe_kv_shape* s, int32_t R, const void* q, const int32
     if (!q || !seq_len || !block_table || !k_cache || !v_cache || !out || !workspace || table_rows < 1 || (!table_row && table_rows < R))
         return MOE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out) || ((uintptr_t)workspace & 255) != 0) return MOE_ERR_INVALID_ARG;
-    const Plan p = plan_of(*s, R);
-    if (workspace_bytes < MOE_ATTN_COUNTER_BYTES + p.parts_bytes) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    size_t need = 0;
+    (void)moe_attn_workspace_bytes(s, R, &need);
+    if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    const Plan p = plan_of(*s, R, table_row != nullptr);
     const int64_t esize = s->dtype == MOE_DTYPE_BF16 ? 2 : 4, row_bytes = (int64_t)R * s->n_q * s->head_dim * esize;
     const int64_t cache_bytes = s->pool_pages * s->page_tokens * s->n_kv * s->head_dim * esize;
     if (overlap(out, row_bytes, q, row_bytes) || overlap(out, row_bytes, k_cache, cache_bytes) || overlap(out, row_bytes, v_cache, cache_bytes) ||
@@ -835,6 +954,7 @@ int moe_attn_decode(const moe_kv_shape* s, int32_t R, const void* q, const int32
     a.n_kv = s->n_kv;
     a.group = s->n_q / s->n_kv;
     a.head_tiles = p.head_tiles;
+    a.pack = p.pack;
     a.P = s->page_tokens;
     a.max_pages = s->max_pages;
     a.table_rows = table_rows;

@@ -361,6 +361,66 @@ def test_attention_prompt_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (2, 1), (3, 1), (4, 1), (5, 1), (6, 2), (7, 1), (8, 1), (16, 2), (32, 8), (9, 1)])
+def test_attention_rows_of_one_request_share_columns(n_q, n_kv, dtype):
+    # 16, 8, 5, 4, 3 and 2 rows to the columns of an MFMA, and one; groups that are cut by the end of a prompt, by rows without a request or without
+    # tokens, at every place; few rows and more than a wavefront looks at; rows of a request out of order and far apart
+    lens = [37, 150, 3, 129]
+    c = Cache(lens, n_kv, 64, 16, dtype, n_q)
+    kv = M.make_kv_shape(n_q, n_kv, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+    rows = [0] * 36 + [1] * 150 + [-1] + [2] * 3 + [-1, -1] + [3] * 129
+    seq = list(range(2, 38)) + list(range(1, 151)) + [7] + [1, 2, 3] + [5, 0] + list(range(1, 130))
+    rows += [1, 1, 1, 1, 0, 1, 1, 1, 1, 1, 1, 1, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3, 3]
+    seq += [150, 1, 77, 0, 30, 5, 140, 32, 33, 64, 31, 0] + [129, 128, 1, 2] * 4 + [64, 96]
+    assert len(rows) == len(seq)
+    q = queries(len(rows), kv, dtype, n_q + 1)
+    for n in (len(rows), 60, 43, 17, 5, 2):
+        for window in (0, 9, 40):
+            attend_and_compare(c, kv, q[:n], seq[:n], dtype, table_row=rows[:n], window=window, rows=range(n) if n < 100 else range(0, n, 3), what=f"{n_q}/{n_kv} {dtype} {n} rows, window {window}")
+
+
+@pytest.mark.parametrize("dtype,D,n_q,n_kv", [("bf16", 128, 4, 1), ("f32", 128, 8, 2), ("bf16", 256, 6, 1), ("bf16", 96, 2, 2), ("f32", 32, 3, 3)])
+def test_attention_long_prompts_are_split_over_blocks(dtype, D, n_q, n_kv):
+    lens = [700, 30, 1500]
+    c = Cache(lens, n_kv, D, 16, dtype, D)
+    kv = M.make_kv_shape(n_q, n_kv, D, 16, c.table.shape[1], c.k.shape[0], dtype)
+    rows = [0] * 20 + [2] * 40 + [1] * 30 + [2] * 7
+    seq = list(range(681, 701)) + list(range(1461, 1501)) + list(range(1, 31)) + list(range(1400, 1407))
+    attend_and_compare(c, kv, queries(97, kv, dtype, 1), seq, dtype, table_row=rows, what=f"D={D} {dtype}")
+    attend_and_compare(c, kv, queries(97, kv, dtype, 2)[:6], seq[:6], dtype, table_row=rows[:6], what=f"D={D} {dtype}, six rows")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_later_tokens_do_not_reach_earlier_rows(dtype):
+    # bad values at tokens that only the later rows of a group see, and in one request of a group of two
+    lens = [60, 50]
+    c = Cache(lens, 2, 64, 16, dtype, 4)
+    kv = M.make_kv_shape(8, 2, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+    rows, seq = [0] * 60 + [1] * 50, list(range(1, 61)) + list(range(1, 51))
+    q = queries(110, kv, dtype, 7)
+    for window in (0, 12):
+        clean, _ = attend_and_compare(c, kv, q, seq, dtype, table_row=rows, window=window)
+        k, v = c.k.clone(), c.v.clone()
+        v[c.table[0, 1], :, 10, 3] = float("inf")          # token 26 of the first request
+        v[c.table[0, 2], :, 1, 5] = float("nan")           # token 33
+        k[c.table[0, 2], :, 14, 7] = float("nan")          # token 46
+        out, _ = M.moe_attn_decode(kv, q.cuda(), i32(seq), c.table.cuda(), k.cuda(), v.cuda(), table_row=i32(rows), window=window)
+        torch.cuda.synchronize()
+        for r in range(110):
+            n, first = seq[r], max(0, seq[r] - window) if window else 0
+            sees = [t for t in (26, 33, 46) if rows[r] == 0 and first <= t < n]
+            same = torch.ones(64, dtype=torch.bool)
+            if 46 in sees:
+                assert out[r].isnan().all(), r
+                continue
+            for t, d in ((26, 3), (33, 5)):
+                if t in sees:
+                    same[d] = False
+                    assert not out[r, :, d].isfinite().any(), (r, t)
+            assert torch.equal(out[r].cpu()[:, same], clean[r].cpu()[:, same]), r
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_extreme_scores(dtype):
     c = Cache([1, 40, 513], 2, 64, 16, dtype, 9, std=30.0)
     kv = M.make_kv_shape(4, 2, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
