@@ -421,7 +421,7 @@ int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t 
  *   MOE_ATTN_COUNTER_BYTES must be zero before its first use; every call leaves them zero, for any shape and R.  Two calls
  *   that overlap in time need two.
  * A row's bits depend on how the rows of its call are split, and so on their lengths; equal calls give equal bits.
- * q, out and the cache 16-byte aligned; R * ceil(max_pages * page_tokens / 16) < 2^31. */
+ * q, out and the cache 16-byte aligned; R * ceil(max_pages * page_tokens / 16) < 2^30. */
 #define MOE_ATTN_COUNTER_BYTES 16384
 int moe_attn_workspace_bytes(const moe_kv_shape* s, int32_t R, size_t* bytes);
 int moe_attn_decode(const moe_kv_shape* s, int32_t R, const void* q, const int32_t* seq_len, const int32_t* table_row,

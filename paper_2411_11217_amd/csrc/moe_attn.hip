@@ -867,7 +867,7 @@ int check_rows(const moe_kv_shape* s, int32_t R) {
     int rc = validate_kv(s);
     if (rc != MOE_OK) return rc;
     const int64_t tiles = ((int64_t)s->max_pages * s->page_tokens + 15) / 16;
-    return R < 0 || R * tiles > INT32_MAX ? MOE_ERR_INVALID_ARG : MOE_OK;
+    return R < 0 || R * tiles >= (int64_t)1 << 30 ? MOE_ERR_INVALID_ARG : MOE_OK;      // tiles are counted in 32 bits, up to a block's share beyond the last
 }
 
 template <class Elem, int D, bool ONCE, bool PACKED>

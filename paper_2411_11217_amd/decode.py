@@ -51,20 +51,20 @@ class DecodeLayers:
         self.lengths = torch.zeros(self.n_requests, dtype=torch.int32, device=device)
         self.free_head = torch.zeros(1, dtype=torch.int32, device=device)
         self.status = torch.zeros(4, dtype=torch.int32, device=device)
-        self._steps = {}                                  # rows -> two KvSteps and whose turn it is
-        self._workspaces = {}                             # rows -> AttnWorkspace
+        self._rows, self._pair, self._turn = -1, (), 0    # two KvSteps for the number of rows of the step before, taken in turn
+        self._workspace: Optional[B.AttnWorkspace] = None
 
     def step(self, embedded: torch.Tensor, fresh: torch.Tensor) -> Tuple[torch.Tensor, B.KvStep]:
         """embedded float32 [T, H]: the fresh tokens of all requests, in the order of the requests; fresh int32 [n_requests].
         -> (hidden states float32 [T, H] after the last layer, the step's tables).  Nothing waits for the device: a request that does
         not fit (bits 1 and 2 of status[0]) keeps its length, and its rows of the result mean nothing."""
         kv, T = self.kv, embedded.shape[0]
-        if T not in self._steps:
-            self._steps[T] = [[B.KvStep(kv, self.n_requests, T, embedded.device) for _ in range(2)], 0]
-            self._workspaces[T] = B.AttnWorkspace(kv, T, embedded.device)
-        pair = self._steps[T]
-        tables = pair[0][pair[1]]
-        pair[1] ^= 1
+        if T != self._rows:
+            self._rows, self._pair = T, [B.KvStep(kv, self.n_requests, T, embedded.device) for _ in range(2)]
+        if self._workspace is None or self._workspace.buf.numel() < B.attn_workspace_bytes(kv, T):
+            self._workspace = B.AttnWorkspace(kv, T, embedded.device)
+        tables = self._pair[self._turn]
+        self._turn ^= 1
         B.moe_kv_assign(kv, self.lengths, fresh, self.free_pages, self.free_head, self.block_table, step=tables, status=self.status)
         seen = torch.where(tables.slots >= 0, tables.positions + 1, 0)          # rows without a slot attend to nothing
         s = self.shape.with_tokens(T)
@@ -75,7 +75,7 @@ class DecodeLayers:
             hidden, _, qkv, _ = B.moe_pre_attention(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, want_bf16=False)
             q = B.moe_qk_norm_rope(kv, qkv, self.inv_freq, tables.positions, tables.slots, k_cache, v_cache, w.q_gamma, w.k_gamma, self.eps, status=self.status)
             attn, _ = B.moe_attn_decode(kv, q, seen, self.block_table, k_cache, v_cache, window=self.window, table_row=tables.request,
-                                        workspace=self._workspaces[T], status=self.status)
+                                        workspace=self._workspace, status=self.status)
             hidden, _, delta, _ = B.moe_post_attention(s, o_proj, attn.view(T, self.attn_width), hidden, w.o_table, w.norm_moe, self.eps, w.Wr,
                                                        w.page_table, w.page_pool, bias=w.bias)
         self.lengths, self.free_head = tables.seq_len, tables.free_head

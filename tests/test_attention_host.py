@@ -101,6 +101,8 @@ def test_attention_refusals_and_workspace():
     assert lib.moe_attn_workspace_bytes(ctypes.byref(s), 5, None) == B.ERR_INVALID_ARG
     wide = kv(max_pages=(1 << 27) - 1)
     assert lib.moe_attn_workspace_bytes(ctypes.byref(wide), 17, ctypes.byref(ctypes.c_size_t())) == B.ERR_INVALID_ARG        # 17 * 2^27 tiles
+    assert lib.moe_attn_workspace_bytes(ctypes.byref(wide), 9, ctypes.byref(ctypes.c_size_t())) == B.ERR_INVALID_ARG         # 9 rows of 2^27 - 1 tiles
+    assert lib.moe_attn_workspace_bytes(ctypes.byref(wide), 8, ctypes.byref(ctypes.c_size_t())) == 0
     assert lib.moe_attn_workspace_bytes(ctypes.byref(kv(dtype="bf16", head_dim=256, n_q=1024, n_kv=1)), 100000, ctypes.byref(ctypes.c_size_t())) == 0
 
 
