@@ -683,6 +683,17 @@ class KvShape(ctypes.Structure):
         """Of K and of V: [pool_pages, n_kv, page_tokens, head_dim]."""
         return (self.pool_pages, self.n_kv, self.page_tokens, self.head_dim)
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_known", None)
+        super().__setattr__(name, value)
+
+    def known(self):
+        """(reference, dtype, cache shape, n_q, head_dim) for the calls, which are as short as the reading of these fields: kept until a field is set."""
+        k = self.__dict__.get("_known")
+        if k is None:
+            k = self.__dict__["_known"] = (ctypes.byref(self), self.torch_dtype, self.cache_shape, self.n_q, self.head_dim)
+        return k
+
 
 def make_kv_shape(n_q, n_kv, head_dim, page_tokens, max_pages, pool_pages, dtype) -> KvShape:
     code = {"f32": 0, "bf16": 1, torch.float32: 0, torch.bfloat16: 1, 0: 0, 1: 1}[dtype]
@@ -733,12 +744,12 @@ def moe_kv_assign(kv: KvShape, cached, fresh, free_pages, free_head, block_table
         raise ValueError(f"step: made for {step.B} requests, got {B}")
     pc = _dev(cached, torch.int32, (B,), "cached")
     pf = _dev(fresh, torch.int32, (B,), "fresh")
-    pp = _dev(free_pages, torch.int32, (free_pages.shape[0],), "free_pages")
+    pp = _dev(free_pages, torch.int32, None, "free_pages")
     ph = _dev(free_head, torch.int32, (1,), "free_head")
     pt = _dev(block_table, torch.int32, (B, kv.max_pages), "block_table")
-    ps = _dev(status, torch.int32, (4,), "status")
+    ps = None if status is None else _dev(status, torch.int32, (4,), "status")
     o = step._ptrs
-    _check(_lib().moe_kv_assign(ctypes.byref(kv), B, step.T, pc, pf, pp, free_pages.shape[0], ph, pt, o[0], o[1], o[2], o[3], o[4], o[5], ps,
+    _check(_lib().moe_kv_assign(kv.known()[0], B, step.T, pc, pf, pp, free_pages.numel(), ph, pt, o[0], o[1], o[2], o[3], o[4], o[5], ps,
                                 _stream(stream)), "moe_kv_assign")
     return step
 
@@ -748,24 +759,25 @@ def moe_qk_norm_rope(kv: KvShape, qkv, inv_freq, positions, slots, k_cache, v_ca
     """qkv float32 or bf16 [T, n >= (n_q + 2 n_kv) * head_dim]; inv_freq float64 [rot_dim / 2].  -> q dtype [T, n_q, head_dim];
     keys and values go to the cache."""
     T, n = qkv.shape
-    dt = kv.torch_dtype
-    if qkv.dtype is not torch.bfloat16 and qkv.dtype is not torch.float32:
+    ref, dt, cache_shape, n_q, head_dim = kv.known()
+    code = DTYPE_F32 if qkv.dtype is torch.float32 else DTYPE_BF16
+    if code == DTYPE_BF16 and qkv.dtype is not torch.bfloat16:
         raise TypeError(f"qkv: expected torch.float32 or torch.bfloat16, got {qkv.dtype}")
     px = _dev(qkv, qkv.dtype, None, "qkv")
-    pi = _dev(inv_freq, torch.float64, (inv_freq.shape[0],), "inv_freq")
+    pi = _dev(inv_freq, torch.float64, None, "inv_freq")
     pp = _dev(positions, torch.int32, (T,), "positions")
     ps = _dev(slots, torch.int32, (T,), "slots")
-    pk = _dev(k_cache, dt, kv.cache_shape, "k_cache")
-    pv = _dev(v_cache, dt, kv.cache_shape, "v_cache")
-    gq = _dev(q_gamma, torch.float32, (kv.head_dim,), "q_gamma")
-    gk = _dev(k_gamma, torch.float32, (kv.head_dim,), "k_gamma")
-    pst = _dev(status, torch.int32, (4,), "status")
+    pk = _dev(k_cache, dt, cache_shape, "k_cache")
+    pv = _dev(v_cache, dt, cache_shape, "v_cache")
+    gq = None if q_gamma is None else _dev(q_gamma, torch.float32, (head_dim,), "q_gamma")
+    gk = None if k_gamma is None else _dev(k_gamma, torch.float32, (head_dim,), "k_gamma")
+    pst = None if status is None else _dev(status, torch.int32, (4,), "status")
     if q is None:
         with _on(stream):
-            q = torch.empty((T, kv.n_q, kv.head_dim), dtype=dt, device=qkv.device)
-    pq = _dev(q, dt, (T, kv.n_q, kv.head_dim), "q")
-    _check(_lib().moe_qk_norm_rope(ctypes.byref(kv), T, px, DTYPE_BF16 if qkv.dtype is torch.bfloat16 else DTYPE_F32, n, gq, gk, eps, pi,
-                                   2 * inv_freq.shape[0], 1 if pairs else 0, pp, ps, pq, pk, pv, pst, _stream(stream)), "moe_qk_norm_rope")
+            q = torch.empty((T, n_q, head_dim), dtype=dt, device=qkv.device)
+    pq = _dev(q, dt, (T, n_q, head_dim), "q")
+    _check(_lib().moe_qk_norm_rope(ref, T, px, code, n, gq, gk, eps, pi, 2 * inv_freq.numel(), 1 if pairs else 0, pp, ps, pq, pk, pv, pst,
+                                   _stream(stream)), "moe_qk_norm_rope")
     return q
 
 
@@ -794,23 +806,23 @@ def moe_attn_decode(kv: KvShape, q, seq_len, block_table, k_cache, v_cache, scal
                     workspace: Optional[AttnWorkspace] = None, status=None, stream=None):
     """-> (out dtype [R, n_q, head_dim], lse float32 [R, n_q] or None); scale None: 1 / sqrt(head_dim)."""
     R = q.shape[0]
-    dt = kv.torch_dtype
-    shape = (R, kv.n_q, kv.head_dim)
+    ref, dt, cache_shape, n_q, head_dim = kv.known()
+    shape = (R, n_q, head_dim)
     pq = _dev(q, dt, shape, "q")
     pl = _dev(seq_len, torch.int32, (R,), "seq_len")
-    pr = _dev(table_row, torch.int32, (R,), "table_row")
-    pt = _dev(block_table, torch.int32, (block_table.shape[0], kv.max_pages), "block_table")
-    pk = _dev(k_cache, dt, kv.cache_shape, "k_cache")
-    pv = _dev(v_cache, dt, kv.cache_shape, "v_cache")
-    ps = _dev(status, torch.int32, (4,), "status")
+    pr = None if table_row is None else _dev(table_row, torch.int32, (R,), "table_row")
+    table_rows = block_table.shape[0]
+    pt = _dev(block_table, torch.int32, (table_rows, kv.max_pages), "block_table")
+    pk = _dev(k_cache, dt, cache_shape, "k_cache")
+    pv = _dev(v_cache, dt, cache_shape, "v_cache")
+    ps = None if status is None else _dev(status, torch.int32, (4,), "status")
     if out is None or workspace is None or (want_lse and lse is None):
         with _on(stream):
             out = torch.empty(shape, dtype=dt, device=q.device) if out is None else out
             lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device) if want_lse and lse is None else lse
             workspace = AttnWorkspace(kv, R, q.device) if workspace is None else workspace
     po = _dev(out, dt, shape, "out")
-    ple = _dev(lse, torch.float32, shape[:2], "lse")
-    _check(_lib().moe_attn_decode(ctypes.byref(kv), R, pq, pl, pr, pt, block_table.shape[0], pk, pv, int(window),
-                                  kv.head_dim ** -0.5 if scale is None else scale, po, ple, workspace.buf.data_ptr(), workspace.buf.numel(), ps,
-                                  _stream(stream)), "moe_attn_decode")
+    ple = None if lse is None else _dev(lse, torch.float32, shape[:2], "lse")
+    _check(_lib().moe_attn_decode(ref, R, pq, pl, pr, pt, table_rows, pk, pv, int(window), head_dim ** -0.5 if scale is None else scale, po, ple,
+                                  workspace.buf.data_ptr(), workspace.buf.numel(), ps, _stream(stream)), "moe_attn_decode")
     return out, lse

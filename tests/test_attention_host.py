@@ -118,6 +118,11 @@ def test_binding_checks_before_the_library():
     with pytest.raises(ValueError, match="q"):
         M.moe_attn_decode(s, torch.zeros((2, 8, 64), dtype=torch.bfloat16), None, None, None, None)
     assert M.make_kv_shape(8, 2, 64, 16, 8, 100, "f32").cache_shape == (100, 2, 16, 64)
+    # what the calls read is that of the fields, also after one is set
+    s = M.make_kv_shape(8, 2, 64, 16, 8, 100, "f32")
+    assert s.known()[1:] == (torch.float32, (100, 2, 16, 64), 8, 64) and s.known()[0] is s.known()[0]
+    s.head_dim, s.dtype = 128, 1
+    assert s.known()[1:] == (torch.bfloat16, (100, 2, 16, 128), 8, 128)
 
 
 def test_oracle_tables_by_hand():
