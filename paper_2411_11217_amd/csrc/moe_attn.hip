@@ -18,8 +18,8 @@
 // For the second product the lane needs values of exactly these tokens, as A operand one element d per MFMA: it loads
 // d-chunk r of each of its four tokens, whole rows per instruction, and the transposition into pairs of tokens stays
 // inside the lane (v_perm).  So the weights never leave the lane that computed them, and only maxima cross the four lane groups.
-//   bf16: 32 tokens are the 32 steps of one 16x16x32 MFMA.  The weights are split into two bf16 parts, 16 bits of each weight: half
-// a bf16 step on the weights would show in the outputs.  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded.
+//   bf16: 32 tokens are the 32 steps of one 16x16x32 MFMA.  The weights are split into three bf16 parts of 8 bits, all 24 of a float32 weight, so
+// nothing is rounded.  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded either.
 //   The matrix cores are busy a quarter of the time (131001 tokens, 48 heads), so the columns that fewer than 16 heads leave empty cost nothing.
 //
 // us in a graph, and what of the bytes that is (a load-only kernel reads 6.2 TB/s here, 7.1 with the non-temporal hint; an empty launch takes 2):
@@ -562,44 +562,49 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
             // whatever a repeated or later token holds is not always 0.
             auto add_values = [&](bool all, int from_t, int to_t, auto some_c, bool mine) __attribute__((always_inline)) {
                 constexpr bool some = decltype(some_c)::value;
-                uint32_t v[SUB][4][ND];
+                uint32_t seen[SUB][4];                       // all bits or none
 #pragma unroll
                 for (int u = 0; u < SUB; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int d = 0; d < ND; ++d) v[u][i][d] = vf[u][i][d];
-                if (!all) {
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int t = now.t0 + u * 16 + g * 4 + i;
-                            const bool seen = t >= from_t && t < to_t;
-#pragma unroll
-                            for (int d = 0; d < ND; ++d) v[u][i][d] = seen ? v[u][i][d] : 0;
-                        }
-                }
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = now.t0 + u * 16 + g * 4 + i;
+                        seen[u][i] = t >= from_t && t < to_t ? ~0u : 0u;
+                    }
                 if constexpr (SUB == 2) {
-                    u32x4 hi, lo;
+                    u32x4 part[3];
+                    uint32_t both[4];                        // of two tokens, as their values are paired
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int i = 0; i < 4; i += 2) {
-                            const uint32_t p0 = __float_as_uint(sc[u][i]), p1 = __float_as_uint(sc[u][i + 1]);
-                            hi[u * 2 + i / 2] = high_halves(p0, p1);
-                            const float r0 = sc[u][i] - __uint_as_float(p0 & 0xffff0000u), r1 = sc[u][i + 1] - __uint_as_float(p1 & 0xffff0000u);
-                            lo[u * 2 + i / 2] = high_halves(__float_as_uint(r0), __float_as_uint(r1));
+                            float p0 = sc[u][i], p1 = sc[u][i + 1];
+#pragma unroll
+                            for (int n = 0; n < 3; ++n) {
+                                const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+                                part[n][u * 2 + i / 2] = high_halves(b0, b1);
+                                p0 -= __uint_as_float(b0 & 0xffff0000u);
+                                p1 -= __uint_as_float(b1 & 0xffff0000u);
+                            }
+                            both[u * 2 + i / 2] = low_halves(seen[u][i], seen[u][i + 1]);
                         }
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
-                        const u32x4 even = {low_halves(v[0][0][d], v[0][1][d]), low_halves(v[0][2][d], v[0][3][d]),
-                                            low_halves(v[1][0][d], v[1][1][d]), low_halves(v[1][2][d], v[1][3][d])};
-                        const u32x4 odd = {high_halves(v[0][0][d], v[0][1][d]), high_halves(v[0][2][d], v[0][3][d]),
-                                           high_halves(v[1][0][d], v[1][1][d]), high_halves(v[1][2][d], v[1][3][d])};
-                        f32x4 x = scores(uint16_t{}, even, hi, acc[d * 2]), y = scores(uint16_t{}, odd, hi, acc[d * 2 + 1]);
-                        x = scores(uint16_t{}, even, lo, x);
-                        y = scores(uint16_t{}, odd, lo, y);
+                        u32x4 even = {low_halves(vf[0][0][d], vf[0][1][d]), low_halves(vf[0][2][d], vf[0][3][d]),
+                                      low_halves(vf[1][0][d], vf[1][1][d]), low_halves(vf[1][2][d], vf[1][3][d])};
+                        u32x4 odd = {high_halves(vf[0][0][d], vf[0][1][d]), high_halves(vf[0][2][d], vf[0][3][d]),
+                                     high_halves(vf[1][0][d], vf[1][1][d]), high_halves(vf[1][2][d], vf[1][3][d])};
+                        if (!all)
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) {
+                                even[n] &= both[n];
+                                odd[n] &= both[n];
+                            }
+                        f32x4 x = acc[d * 2], y = acc[d * 2 + 1];
+#pragma unroll
+                        for (int n = 0; n < 3; ++n) {
+                            x = scores(uint16_t{}, even, part[n], x);
+                            y = scores(uint16_t{}, odd, part[n], y);
+                        }
                         acc[d * 2] = !some || mine ? x : acc[d * 2];
                         acc[d * 2 + 1] = !some || mine ? y : acc[d * 2 + 1];
                     }
@@ -608,7 +613,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                     for (int d = 0; d < ND; ++d) {
                         f32x4 x = acc[d];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][i][d]), sc[0][i], x, 0, 0, 0);
+                        for (int i = 0; i < 4; ++i)
+                            x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(all ? vf[0][i][d] : vf[0][i][d] & seen[0][i]), sc[0][i], x, 0, 0, 0);
                         acc[d] = !some || mine ? x : acc[d];
                     }
                 }
@@ -642,12 +648,14 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 } else {
                     const int slot = wave * 2 + (begins ? 1 : 0);
                     float* part = slot_of(slot);
-                    if (r < H) {
+                    int col = r;
+                    asm("" : "+v"(col));                     // the addresses are formed here: kept through the loop they would be the registers it lacks
+                    if (col < H) {
 #pragma unroll
-                        for (int e = 0; e < E; ++e) reinterpret_cast<f32x4*>(part)[e * 4 * H + g * H + r] = acc[e];
+                        for (int e = 0; e < E; ++e) reinterpret_cast<f32x4*>(part)[e * 4 * H + g * H + col] = acc[e];
                         if (g == 0) {
-                            part[H * D + r] = m;
-                            part[H * D + H + r] = l;
+                            part[H * D + col] = m;
+                            part[H * D + H + col] = l;
                         }
                     }
                     if (lane == 0) s_split[slot] = Split{now.row, now.start, now.tiles, now.cols, ends ? 1 : 0};
