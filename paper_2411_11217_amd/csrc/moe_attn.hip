@@ -19,7 +19,9 @@
 // d-chunk r of each of its four tokens, whole rows per instruction, and the transposition into pairs of tokens stays
 // inside the lane (v_perm).  So the weights never leave the lane that computed them, and only maxima cross the four lane groups.
 //   bf16: 32 tokens are the 32 steps of one 16x16x32 MFMA.  The weights are split into three bf16 parts of 8 bits, all 24 of a float32 weight, so
-// nothing is rounded.  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded either.
+// nothing is rounded.  A part of 0 would make 0 * infinity of an infinite value, so no part of a weight that is not 0 is 0: the
+// first is the largest number of 8 bits below the weight, the second that below what is left, the third the rest (1 to 256
+// units of the weight's last place).  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded either.
 //   The matrix cores are busy a quarter of the time (131001 tokens, 48 heads), so the columns that fewer than 16 heads leave empty cost nothing.
 //
 // us in a graph, and what of the bytes that is (a load-only kernel reads 6.2 TB/s here, 7.1 with the non-temporal hint; an empty launch takes 2):
@@ -580,7 +582,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                             float p0 = sc[u][i], p1 = sc[u][i + 1];
 #pragma unroll
                             for (int n = 0; n < 3; ++n) {
-                                const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+                                // the largest part below what is left, for the last one what is left: none of a weight's parts is 0, unless the weight is
+                                const uint32_t b0 = __builtin_elementwise_sub_sat(__float_as_uint(p0), n < 2 ? 1u : 0u), b1 = __builtin_elementwise_sub_sat(__float_as_uint(p1), n < 2 ? 1u : 0u);
                                 part[n][u * 2 + i / 2] = high_halves(b0, b1);
                                 p0 -= __uint_as_float(b0 & 0xffff0000u);
                                 p1 -= __uint_as_float(b1 & 0xffff0000u);

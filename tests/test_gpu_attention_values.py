@@ -50,3 +50,96 @@ def test_attention_weights_have_all_bits_of_float32(dtype, share):
     worst = (np.abs(f64(out) - ref) / room).max()
     say(f"    {dtype} share={share}: {worst:.3f} of what is allowed")
     assert worst <= 1.0
+
+
+# ---------------------------------------------------------------------------- infinite values
+
+def compare_infinite(c, kv, q, seq, dtype, places, window=0, table_row=None):
+    """places: (request, token, element, value) put into V in every key/value head.  Elements where a row sees none of them keep their bits; where it does, they are what the
+    definition gives: the infinity that it sees, or no number where it sees both."""
+    P, dev = c.P, (c.table.cuda(), c.k.cuda())
+    rows = None if table_row is None else i32(table_row)
+    clean, lse = M.moe_attn_decode(kv, q.cuda(), i32(seq), *dev, c.v.cuda(), window=window, table_row=rows, want_lse=True)
+    v = c.v.clone()
+    for b, t, d, value in places:
+        v[c.table[b, t // P].long(), :, t % P, d] = value
+    out, lse2 = M.moe_attn_decode(kv, q.cuda(), i32(seq), *dev, v.cuda(), window=window, table_row=rows, want_lse=True)
+    torch.cuda.synchronize()
+    want = clean.float().cpu()
+    assert want.isfinite().all() and torch.equal(lse, lse2)
+    for r, n in enumerate(seq):
+        request = r if table_row is None else table_row[r]
+        first = max(0, n - window) if window else 0
+        for d in {d for _, _, d, _ in places}:
+            seen = [x for b, t, e, x in places if b == request and e == d and first <= t < n]
+            if seen:
+                want[r, :, d] = sum(seen)
+    got = out.float().cpu()
+    same = (got == want) | (got.isnan() & want.isnan())
+    assert same.all(), (got[~same][:8], want[~same][:8], torch.nonzero(~same)[:8])
+
+
+INF = float("inf")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_attention_gives_the_infinity_of_a_value(D, dtype):
+    lens = [1, 1, 2, 17, 33, 64, 300]
+    c = Cache(lens, 2, D, 16, dtype, D)
+    kv = M.make_kv_shape(6, 2, D, 16, c.table.shape[1], c.k.shape[0], dtype)
+    q = queries(len(lens), kv, dtype, D + 1, std=0.5)
+    places = [(0, 0, 3, INF), (1, 0, D - 1, -INF), (2, 1, 0, INF), (2, 0, 5, -INF), (3, 16, 7, INF), (4, 0, 9, -INF), (4, 32, 9, -INF), (5, 40, 11, INF), (5, 3, 11, -INF),
+              (6, 299, 1, INF), (6, 0, 2, -INF), (6, 150, 4, INF), (6, 151, 4, INF)]
+    for window in (0, 20):
+        compare_infinite(c, kv, q, lens, dtype, places, window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scores", ["equal", "powers"])
+def test_attention_gives_the_infinity_of_a_value_whatever_its_weight(dtype, scores):
+    # every token of a request once: weights of exactly 1, and of about 2^-j down to the least that an exponential has
+    n, D = 124, 64
+    c = Cache([n] * n, 1, D, 16, dtype, 5)
+    c.k = torch.zeros_like(c.k)
+    if scores == "powers":
+        t = torch.arange(n)
+        for b in range(n):
+            c.k[c.table[b, t // 16].long(), 0, t % 16, 0] = -t.to(c.k.dtype)
+    kv = M.make_kv_shape(3, 1, D, 16, c.table.shape[1], c.k.shape[0], dtype)
+    q = torch.zeros((n, 3, D), dtype=DT[dtype])
+    q[..., 0] = 0.69140625                       # just below ln 2: token t weighs about 2^-t
+    seq = [n] * n
+    v = c.v.clone()
+    for b in range(n):
+        v[c.table[b, b // 16].long(), :, b % 16, 7] = INF
+    for rows in (None, i32(list(range(n)))):
+        out, _ = M.moe_attn_decode(kv, q.cuda(), i32(seq), c.table.cuda(), c.k.cuda(), v.cuda(), scale=1.0, table_row=rows)
+        torch.cuda.synchronize()
+        assert (out[:, :, 7] == INF).all(), (out[:, 0, 7] != INF).nonzero().flatten().tolist()
+        others = torch.ones(D, dtype=torch.bool)
+        others[7] = False
+        assert out[:, :, others].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (4, 1), (16, 2), (32, 8), (9, 1), (24, 1)])
+def test_attention_gives_the_infinity_of_a_value_in_prompts(n_q, n_kv, dtype):
+    lens = [37, 90, 3]
+    c = Cache(lens, n_kv, 64, 16, dtype, n_q)
+    kv = M.make_kv_shape(n_q, n_kv, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+    rows = [0] * 37 + [-1] + [1] * 90 + [2] * 3
+    seq = list(range(1, 38)) + [0] + list(range(1, 91)) + [1, 2, 3]
+    q = queries(len(rows), kv, dtype, n_q + 1, std=0.5)
+    places = [(0, 0, 3, INF), (0, 20, 8, -INF), (0, 33, 8, INF), (1, 64, 5, INF), (1, 40, 5, INF), (1, 89, 6, -INF), (1, 0, 7, -INF), (2, 2, 1, INF)]
+    for window in (0, 11):
+        compare_infinite(c, kv, q, seq, dtype, places, window, rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_gives_the_infinity_of_a_value_over_many_blocks(dtype):
+    lens = [9000, 2500, 40]
+    c = Cache(lens, 2, 128, 16, dtype, 3)
+    kv = M.make_kv_shape(8, 2, 128, 16, c.table.shape[1], c.k.shape[0], dtype)
+    q = queries(3, kv, dtype, 4, std=0.5)
+    compare_infinite(c, kv, q, lens, dtype, [(0, 0, 1, INF), (0, 8999, 2, -INF), (0, 4000, 3, INF), (0, 7000, 3, -INF), (1, 1200, 100, INF), (1, 1201, 101, -INF), (2, 39, 9, INF)])
