@@ -683,16 +683,17 @@ class KvShape(ctypes.Structure):
         """Of K and of V: [pool_pages, n_kv, page_tokens, head_dim]."""
         return (self.pool_pages, self.n_kv, self.page_tokens, self.head_dim)
 
-    def __setattr__(self, name, value):
-        self.__dict__.pop("_known", None)
-        super().__setattr__(name, value)
+    def __reduce__(self):                            # a copy has the fields, and nothing that was kept for the calls
+        return type(self), tuple(getattr(self, name) for name, _ in self._fields_)
 
     def known(self):
-        """(reference, dtype, cache shape, n_q, head_dim) for the calls, which are as short as the reading of these fields: kept until a field is set."""
-        k = self.__dict__.get("_known")
-        if k is None:
-            k = self.__dict__["_known"] = (ctypes.byref(self), self.torch_dtype, self.cache_shape, self.n_q, self.head_dim)
-        return k
+        """(reference, dtype, cache shape, n_q, head_dim) for the calls, which are as short as the reading of these fields: kept as long as
+        the bytes of the structure are the same, whoever writes them."""
+        now = bytes(self)
+        kept = self.__dict__.get("_known")
+        if kept is None or kept[0] != now:
+            kept = self.__dict__["_known"] = (now, (ctypes.byref(self), self.torch_dtype, self.cache_shape, self.n_q, self.head_dim))
+        return kept[1]
 
 
 def make_kv_shape(n_q, n_kv, head_dim, page_tokens, max_pages, pool_pages, dtype) -> KvShape:

@@ -1,0 +1,52 @@
+"""Handles of the attention's calls on the host: shapes of a cache and tables of a step that are copied, pickled or changed stay their
+own, and what reaches the library is what the handle of the call says."""
+import copy
+import ctypes
+import pickle
+
+import pytest
+import torch
+
+import paper_2411_11217_amd as M
+from paper_2411_11217_amd import binding as B
+
+FIELDS = [n for n, _ in B.KvShape._fields_]
+
+
+def values(kv):
+    return [getattr(kv, n) for n in FIELDS]
+
+
+def told(kv):
+    """What a call tells the library: the structure behind the reference, and what the binding checks tensors against."""
+    ref, dtype, cache_shape, n_q, head_dim = kv.known()
+    assert (dtype, cache_shape, n_q, head_dim) == (kv.torch_dtype, kv.cache_shape, kv.n_q, kv.head_dim)
+    return values(ctypes.cast(ref, ctypes.POINTER(B.KvShape)).contents)
+
+
+@pytest.mark.parametrize("used", [False, True])
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, lambda s: pickle.loads(pickle.dumps(s)), lambda s: B.KvShape.from_buffer_copy(s), lambda s: copy.copy(copy.deepcopy(s))])
+def test_a_copied_shape_is_its_own(how, used):
+    s = M.make_kv_shape(8, 2, 64, 16, 8, 100, "bf16")
+    if used:
+        s.known()
+    c = how(s)
+    assert type(c) is B.KvShape and values(c) == values(s)
+    s.pool_pages, s.max_pages, s.head_dim = 1000000, 3, 128
+    assert told(c) == [8, 2, 64, 16, 8, 1, 100] and told(s) == [8, 2, 128, 16, 3, 1, 1000000]
+    c.dtype, c.page_tokens = 0, 5
+    assert told(c) == [8, 2, 64, 5, 8, 0, 100] and told(s) == [8, 2, 128, 16, 3, 1, 1000000]
+    d = how(c)                                   # and after both have been used
+    c.n_q = 4
+    assert told(d) == [8, 2, 64, 5, 8, 0, 100] and told(c) == [4, 2, 64, 5, 8, 0, 100]
+
+
+def test_a_shape_changed_through_other_memory_is_read_again():
+    s = M.make_kv_shape(8, 2, 64, 16, 8, 100, "bf16")
+    assert s.known()[0] is s.known()[0]
+    same = B.KvShape.from_buffer(s)
+    s.known()
+    same.pool_pages, same.dtype = 7, 0
+    assert told(s) == [8, 2, 64, 16, 8, 0, 7] and told(same) == told(s)
+    ctypes.pointer(s).contents.head_dim = 32
+    assert told(s)[2] == 32 and told(same)[2] == 32
