@@ -728,8 +728,6 @@ class KvStep:
         self.buf = torch.zeros(at, dtype=torch.int32, device=device)
         for (name, n), o in zip(sizes, starts):
             setattr(self, name, self.buf[o:o + n])
-        base = self.buf.data_ptr()
-        self._ptrs = [base + 4 * o for o in starts]
 
 
 def moe_kv_assign(kv: KvShape, cached, fresh, free_pages, free_head, block_table, step: Optional[KvStep] = None, T: Optional[int] = None,
@@ -749,9 +747,8 @@ def moe_kv_assign(kv: KvShape, cached, fresh, free_pages, free_head, block_table
     ph = _dev(free_head, torch.int32, (1,), "free_head")
     pt = _dev(block_table, torch.int32, (B, kv.max_pages), "block_table")
     ps = None if status is None else _dev(status, torch.int32, (4,), "status")
-    o = step._ptrs
-    _check(_lib().moe_kv_assign(kv.known()[0], B, step.T, pc, pf, pp, free_pages.numel(), ph, pt, o[0], o[1], o[2], o[3], o[4], o[5], ps,
-                                _stream(stream)), "moe_kv_assign")
+    _check(_lib().moe_kv_assign(kv.known()[0], B, step.T, pc, pf, pp, free_pages.numel(), ph, pt, step.seq_len.data_ptr(), step.row_start.data_ptr(),
+                                step.positions.data_ptr(), step.slots.data_ptr(), step.request.data_ptr(), step.free_head.data_ptr(), ps, _stream(stream)), "moe_kv_assign")
     return step
 
 

@@ -50,3 +50,39 @@ def test_a_shape_changed_through_other_memory_is_read_again():
     assert told(s) == [8, 2, 64, 16, 8, 0, 7] and told(same) == told(s)
     ctypes.pointer(s).contents.head_dim = 32
     assert told(s)[2] == 32 and told(same)[2] == 32
+
+
+# ---------------------------------------------------------------------------- tables of a step
+
+OUTPUTS = ("seq_len", "row_start", "positions", "slots", "request", "free_head")
+
+
+class Recorder:
+    """In place of the library: keeps the arguments of moe_kv_assign."""
+
+    def __init__(self, monkeypatch):
+        self.calls = []
+        monkeypatch.setattr(B, "_lib", lambda: self)
+        monkeypatch.setattr(B, "_dev", lambda t, dtype, shape, name: None if t is None else t.data_ptr())
+        monkeypatch.setattr(B, "_stream", lambda stream: 0)
+
+    def moe_kv_assign(self, *args):
+        self.calls.append(args)
+        return 0
+
+
+@pytest.mark.parametrize("used", [False, True])
+@pytest.mark.parametrize("how", [copy.deepcopy, lambda s: pickle.loads(pickle.dumps(s)), copy.copy, lambda s: s])
+def test_a_copied_step_is_written_where_it_is_read(how, used, monkeypatch):
+    lib = Recorder(monkeypatch)
+    kv = M.make_kv_shape(1, 1, 32, 16, 8, 100, "bf16")
+    args = [torch.zeros(n, dtype=torch.int32) for n in ((3,), (3,), (100,), (1,), (3, 8))]
+    step = B.KvStep(kv, 3, 40, "cpu")
+    if used:
+        B.moe_kv_assign(kv, *args, step=step)
+    other = how(step)
+    assert B.moe_kv_assign(kv, *args, step=other) is other
+    assert list(lib.calls[-1][9:15]) == [getattr(other, name).data_ptr() for name in OUTPUTS]
+    assert lib.calls[-1][1:3] == (3, 40) and [getattr(other, name).numel() for name in OUTPUTS] == [3, 4, 40, 40, 40, 1]
+    B.moe_kv_assign(kv, *args, step=step)
+    assert list(lib.calls[-1][9:15]) == [getattr(step, name).data_ptr() for name in OUTPUTS]
