@@ -136,7 +136,7 @@ def _check(status: int, where: str):
 def _stream(stream) -> int:
     if stream is None:
         # the current stream's handle, without a Stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 

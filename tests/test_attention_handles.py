@@ -86,3 +86,15 @@ def test_a_copied_step_is_written_where_it_is_read(how, used, monkeypatch):
     assert lib.calls[-1][1:3] == (3, 40) and [getattr(other, name).numel() for name in OUTPUTS] == [3, 4, 40, 40, 40, 1]
     B.moe_kv_assign(kv, *args, step=step)
     assert list(lib.calls[-1][9:15]) == [getattr(step, name).data_ptr() for name in OUTPUTS]
+
+
+# ---------------------------------------------------------------------------- streams
+
+def test_the_current_device_is_asked_for_by_its_public_name(monkeypatch):
+    # torch.cuda.current_device initialises the device, and refuses in a child that was forked from a process that has
+    asked = []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: asked.append("device") or 3)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 1000 + device, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 5, raising=False)
+    assert B._stream(None) == 1003 and asked == ["device"]
+    assert B._stream(77) == 77
