@@ -57,14 +57,14 @@ class DecodeLayers:
     def step(self, embedded: torch.Tensor, fresh: torch.Tensor) -> Tuple[torch.Tensor, B.KvStep]:
         """embedded float32 [T, H]: the fresh tokens of all requests, in the order of the requests; fresh int32 [n_requests].
         -> (hidden states float32 [T, H] after the last layer, the step's tables).  Nothing waits for the device: a request that does
-        not fit (bits 1 and 2 of status[0]) keeps its length, and its rows of the result mean nothing."""
+        not fit (bits 1 and 2 of status[0]) keeps its length, and its rows of the result mean nothing.  The tables are written again two
+        steps later.  A call that raises leaves the requests as they were, and the step can be taken again."""
         kv, T = self.kv, embedded.shape[0]
         if T != self._rows:
             self._rows, self._pair = T, [B.KvStep(kv, self.n_requests, T, embedded.device) for _ in range(2)]
         if self._workspace is None or self._workspace.buf.numel() < B.attn_workspace_bytes(kv, T):
             self._workspace = B.AttnWorkspace(kv, T, embedded.device)
-        tables = self._pair[self._turn]
-        self._turn ^= 1
+        tables = self._pair[self._turn]              # not the one that holds self.lengths: _turn goes on with them
         B.moe_kv_assign(kv, self.lengths, fresh, self.free_pages, self.free_head, self.block_table, step=tables, status=self.status)
         seen = torch.where(tables.slots >= 0, tables.positions + 1, 0)          # rows without a slot attend to nothing
         s = self.shape.with_tokens(T)
@@ -78,5 +78,6 @@ class DecodeLayers:
                                         workspace=self._workspace, status=self.status)
             hidden, _, delta, _ = B.moe_post_attention(s, o_proj, attn.view(T, self.attn_width), hidden, w.o_table, w.norm_moe, self.eps, w.Wr,
                                                        w.page_table, w.page_pool, bias=w.bias)
-        self.lengths, self.free_head = tables.seq_len, tables.free_head
-        return hidden + delta, tables
+        out = hidden + delta
+        self.lengths, self.free_head, self._turn = tables.seq_len, tables.free_head, self._turn ^ 1
+        return out, tables

@@ -1,0 +1,122 @@
+"""What DecodeLayers keeps from step to step, on the host: its calls of the library are replaced by stand-ins on CPU tensors (the
+tables by the oracle's), so that a step can fail at any of them."""
+import types
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_11217_amd as M
+from oracle import attention
+from paper_2411_11217_amd import binding as B
+
+H, P, WIDTH, POOL = 256, 4, 6, 14
+CALLS = ("moe_kv_assign", "moe_pre_attention", "moe_qk_norm_rope", "moe_attn_decode", "moe_post_attention")
+
+
+class Library:
+    """Counts its calls, and fails at the one it is told to."""
+
+    def __init__(self, monkeypatch):
+        self.calls, self.fails = [], None
+        for name in CALLS:
+            monkeypatch.setattr(B, name, self.entry(name))
+        monkeypatch.setattr(B, "AttnWorkspace", lambda kv, R, device: types.SimpleNamespace(buf=torch.zeros(B.attn_workspace_bytes(kv, R), dtype=torch.uint8)))
+
+    def entry(self, name):
+        def call(*args, **kw):
+            self.calls.append(name)
+            out = getattr(self, name)(*args, **kw)         # what was enqueued before an error has been done
+            if self.fails is not None and len(self.calls) == self.fails:
+                raise B.MoEError(B.ERR_INVALID_ARG, name)
+            return out
+        return call
+
+    def moe_kv_assign(self, kv, cached, fresh, free_pages, free_head, block_table, step, status):
+        outs = [getattr(step, n) for n in ("seq_len", "row_start", "positions", "slots", "request", "free_head")]
+        if any(i.data_ptr() == o.data_ptr() for i in (cached, fresh, free_pages, free_head) for o in outs):
+            raise B.MoEError(B.ERR_INVALID_ARG, "moe_kv_assign: an output is an input")
+        r = attention.assign(kv.page_tokens, kv.max_pages, kv.pool_pages, step.T, cached.numpy(), fresh.numpy(), free_pages.numpy(), int(free_head), block_table.numpy())
+        for o, n in zip(outs, ("seq_len", "row_start", "positions", "slots", "request", "free_head")):
+            o.copy_(torch.from_numpy(r[n]))
+        block_table.copy_(torch.from_numpy(r["block_table"]))
+        status[0] |= r["status"]
+
+    def moe_pre_attention(self, qkv_proj, hidden, delta, *rest, want_bf16):
+        hidden = delta if hidden is None else hidden + delta
+        return hidden, None, hidden[:, :96], None
+
+    def moe_qk_norm_rope(self, kv, qkv, inv_freq, positions, slots, k_cache, v_cache, *rest, status):
+        for r, s in enumerate(slots.tolist()):
+            if s >= 0:
+                k_cache[s // P, 0, s % P], v_cache[s // P, 0, s % P] = qkv[r, 32:64].bfloat16(), qkv[r, 64:96].bfloat16()
+        return qkv[:, :32].bfloat16().view(-1, 1, 32)
+
+    def moe_attn_decode(self, kv, q, seen, block_table, k_cache, v_cache, window, table_row, workspace, status):
+        out = torch.zeros_like(q)
+        for r, n in enumerate(seen.tolist()):
+            t = torch.arange(n)
+            if n:
+                out[r, 0] = (q[r, 0] + v_cache[block_table[table_row[r]].long()[t // P], 0, t % P].float().sum(0)).bfloat16()
+        return out, None
+
+    def moe_post_attention(self, s, o_proj, attn, hidden, *rest, bias):
+        return hidden, None, 0.5 * attn.float().repeat(1, H // 32), None
+
+
+def build(n_layers=2, n_requests=3, dtype="bf16"):
+    kv = M.make_kv_shape(1, 1, 32, P, WIDTH, POOL, dtype)
+    s = M.make_shape(1, H, 384, 4, 2, "bf16", 64 * 1024)
+    layers = [M.LayerWeights(*[None] * 7) for _ in range(n_layers)]
+    return M.DecodeLayers(s, kv, layers, torch.zeros(16, dtype=torch.float64), n_requests, device="cpu")
+
+
+def kept(model):
+    return [t.clone() for t in (model.lengths, model.free_head, model.block_table, model.free_pages, model.status)]
+
+
+def tokens(T, seed):
+    return torch.randn((T, H), generator=torch.Generator().manual_seed(seed))
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+STEPS = ([2, 0, 3], [1, 3, 1], [1, 1, 1], [1, 1, 1], [3, 0, 0], [1, 1, 1], [0, 1, 0])
+
+
+@pytest.mark.parametrize("fails", range(1, 10))
+def test_a_step_that_fails_leaves_the_requests_as_they_were(fails, monkeypatch):
+    # every step once with an error at the `fails`-th call of nine, once more at the next, then well: as a model that never failed
+    lib = Library(monkeypatch)
+    one, other = build(), build()
+    for n, fresh in enumerate(STEPS):
+        x = tokens(sum(fresh), n)
+        want, _ = one.step(x, i32(fresh))
+        for at in (fails, fails % 9 + 1):
+            before = kept(other)
+            lib.calls.clear()
+            lib.fails = at
+            with pytest.raises(M.MoEError, match=CALLS[0 if at == 1 else (at - 2) % 4 + 1]):
+                other.step(x, i32(fresh))
+            assert len(lib.calls) == at and torch.equal(before[0], other.lengths) and torch.equal(before[1], other.free_head)
+        lib.fails = None
+        got, tables = other.step(x, i32(fresh))
+        assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(kept(one), kept(other)))
+        assert tables.seq_len.data_ptr() == other.lengths.data_ptr()
+
+
+def test_a_step_whose_last_sum_fails_leaves_the_requests_as_they_were(monkeypatch):
+    lib = Library(monkeypatch)
+    model = build(n_layers=1)
+    model.step(tokens(3, 0), i32([1, 1, 1]))
+    before = kept(model)
+    whole = Library.moe_post_attention
+    monkeypatch.setattr(Library, "moe_post_attention", lambda *a, **kw: (a[4], None, torch.zeros(7, 3), None))
+    with pytest.raises(RuntimeError):
+        model.step(tokens(3, 1), i32([1, 1, 1]))
+    assert torch.equal(before[0], model.lengths) and torch.equal(before[1], model.free_head) and lib.fails is None
+    monkeypatch.setattr(Library, "moe_post_attention", whole)
+    model.step(tokens(3, 1), i32([1, 1, 1]))
+    assert model.lengths.tolist() == [2, 2, 2]
