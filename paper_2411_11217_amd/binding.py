@@ -669,6 +669,9 @@ def moe_pre_attention(qkv_proj: LinearShape, hidden, delta, norm_gamma, eps, qkv
 
 # ----------------------------------------------------------------------------- attention over a paged key-value cache
 
+MAX_REQUESTS = 4096                               # MOE_MAX_REQUESTS
+
+
 class KvShape(ctypes.Structure):
     """struct moe_kv_shape: heads, head size and page geometry of a paged key-value cache."""
     _fields_ = [("n_q", _i32), ("n_kv", _i32), ("head_dim", _i32), ("page_tokens", _i32), ("max_pages", _i32), ("dtype", _i32),

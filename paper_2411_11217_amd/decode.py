@@ -40,10 +40,18 @@ class DecodeLayers:
 
     def __init__(self, shape: B.MoEShape, kv: B.KvShape, layers: Sequence[LayerWeights], inv_freq: torch.Tensor, n_requests: int,
                  eps: float = 1e-5, window: int = 0, device="cuda"):
+        if kv.dtype != B.DTYPE_BF16 or shape.dtype != B.DTYPE_BF16:
+            raise ValueError("DecodeLayers: cache and MoE layer have to be bf16, the type of the projections beside them")
+        if not 0 <= n_requests <= B.MAX_REQUESTS:
+            raise ValueError(f"n_requests: at most {B.MAX_REQUESTS}, got {n_requests}")
         self.shape, self.kv, self.layers, self.n_requests = shape, kv, list(layers), int(n_requests)
         self.inv_freq, self.eps, self.window = inv_freq, float(eps), int(window)
         width = (kv.n_q + 2 * kv.n_kv) * kv.head_dim
         self.qkv_width, self.attn_width = -(-width // 128) * 128, kv.n_q * kv.head_dim
+        for status in (B.kv_validate(kv), B.validate_shape(shape)):
+            B._check(status, "DecodeLayers")
+        for K, N in ((shape.H, self.qkv_width), (self.attn_width, shape.H)):
+            B.linear_pages_required(B.make_linear_shape(1, K, N, shape.page_bytes))         # raises where the projections do not take such sizes
         self.caches: List[Tuple[torch.Tensor, torch.Tensor]] = [
             (torch.empty(kv.cache_shape, dtype=kv.torch_dtype, device=device), torch.empty(kv.cache_shape, dtype=kv.torch_dtype, device=device)) for _ in self.layers]
         self.block_table = torch.full((self.n_requests, kv.max_pages), -1, dtype=torch.int32, device=device)

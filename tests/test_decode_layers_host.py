@@ -44,29 +44,29 @@ class Library:
 
     def moe_pre_attention(self, qkv_proj, hidden, delta, *rest, want_bf16):
         hidden = delta if hidden is None else hidden + delta
-        return hidden, None, hidden[:, :96], None
+        return hidden, None, hidden[:, :192], None
 
     def moe_qk_norm_rope(self, kv, qkv, inv_freq, positions, slots, k_cache, v_cache, *rest, status):
         for r, s in enumerate(slots.tolist()):
             if s >= 0:
-                k_cache[s // P, 0, s % P], v_cache[s // P, 0, s % P] = qkv[r, 32:64].bfloat16(), qkv[r, 64:96].bfloat16()
-        return qkv[:, :32].bfloat16().view(-1, 1, 32)
+                k_cache[s // P, 0, s % P], v_cache[s // P, 0, s % P] = qkv[r, 128:160].bfloat16(), qkv[r, 160:192].bfloat16()
+        return qkv[:, :128].bfloat16().view(-1, 4, 32)
 
     def moe_attn_decode(self, kv, q, seen, block_table, k_cache, v_cache, window, table_row, workspace, status):
         out = torch.zeros_like(q)
         for r, n in enumerate(seen.tolist()):
             t = torch.arange(n)
             if n:
-                out[r, 0] = (q[r, 0] + v_cache[block_table[table_row[r]].long()[t // P], 0, t % P].float().sum(0)).bfloat16()
+                out[r] = (q[r] + v_cache[block_table[table_row[r]].long()[t // P], 0, t % P].float().sum(0)).bfloat16()
         return out, None
 
     def moe_post_attention(self, s, o_proj, attn, hidden, *rest, bias):
-        return hidden, None, 0.5 * attn.float().repeat(1, H // 32), None
+        return hidden, None, 0.5 * attn.float().repeat(1, H // 128), None
 
 
-def build(n_layers=2, n_requests=3, dtype="bf16"):
-    kv = M.make_kv_shape(1, 1, 32, P, WIDTH, POOL, dtype)
-    s = M.make_shape(1, H, 384, 4, 2, "bf16", 64 * 1024)
+def build(n_layers=2, n_requests=3, dtype="bf16", n_q=4, H=H, layer_dtype="bf16", page_bytes=64 * 1024):
+    kv = M.make_kv_shape(n_q, 1, 32, P, WIDTH, POOL, dtype)
+    s = M.make_shape(1, H, 384, 4, 2, layer_dtype, page_bytes)
     layers = [M.LayerWeights(*[None] * 7) for _ in range(n_layers)]
     return M.DecodeLayers(s, kv, layers, torch.zeros(16, dtype=torch.float64), n_requests, device="cpu")
 
@@ -120,3 +120,13 @@ def test_a_step_whose_last_sum_fails_leaves_the_requests_as_they_were(monkeypatc
     monkeypatch.setattr(Library, "moe_post_attention", whole)
     model.step(tokens(3, 1), i32([1, 1, 1]))
     assert model.lengths.tolist() == [2, 2, 2]
+
+
+def test_what_no_step_could_take_is_refused_when_the_layers_are_made(monkeypatch):
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: pytest.fail("memory before the checks"))
+    for kw in (dict(dtype="f32"), dict(layer_dtype="f32")):
+        with pytest.raises(ValueError, match="bf16"):
+            build(**kw)
+    for kw in (dict(n_q=5), dict(n_q=0), dict(H=200), dict(page_bytes=1000), dict(n_requests=4097)):        # 160 values for the O projection, no heads, ..
+        with pytest.raises((ValueError, M.MoEError)):
+            build(**kw)
