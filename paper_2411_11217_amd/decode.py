@@ -89,3 +89,18 @@ class DecodeLayers:
         out = hidden + delta
         self.lengths, self.free_head, self._turn = tables.seq_len, tables.free_head, self._turn ^ 1
         return out, tables
+
+    def retire(self, seats: torch.Tensor) -> None:
+        """seats bool [n_requests]: these requests are done.  Their pages are free again, and their seats are of length 0 for others to take with the
+        next step's fresh tokens.  Nothing waits for the device, as in a step."""
+        if seats.dtype is not torch.bool or seats.shape != (self.n_requests,):
+            raise ValueError(f"seats: expected torch.bool [{self.n_requests}], got {seats.dtype} {list(seats.shape)}")
+        # The pages that are taken are those before free_head: the freed ones go to the last places of these, one after another.
+        held = torch.where(seats, (self.lengths.long() + self.kv.page_tokens - 1) // self.kv.page_tokens, 0)
+        freed = (torch.arange(self.kv.max_pages, device=seats.device) < held[:, None]).flatten()
+        count = held.sum()
+        to = torch.where(freed, self.free_head.long() - count + freed.cumsum(0) - 1, self.kv.pool_pages)         # what stays goes behind the list, and is cut off
+        free_pages = torch.cat([self.free_pages, self.free_pages[:1]]).scatter_(0, to, self.block_table.flatten())[:-1]
+        free_head, lengths = (self.free_head - count).to(torch.int32), self.lengths.masked_fill(seats, 0)
+        self.block_table.masked_fill_(seats[:, None], -1)
+        self.free_pages, self.free_head, self.lengths = free_pages, free_head, lengths

@@ -130,3 +130,62 @@ def test_what_no_step_could_take_is_refused_when_the_layers_are_made(monkeypatch
     for kw in (dict(n_q=5), dict(n_q=0), dict(H=200), dict(page_bytes=1000), dict(n_requests=4097)):        # 160 values for the O projection, no heads, ..
         with pytest.raises((ValueError, M.MoEError)):
             build(**kw)
+
+
+# ---------------------------------------------------------------------------- requests that are done
+
+def pages_are_whole(model):
+    """Every page of the pool is held by one request or free, once; behind a request's pages its row is of no concern."""
+    held = [p for b, n in enumerate(model.lengths.tolist()) for p in model.block_table[b, :-(-n // P)].tolist()]
+    assert sorted(held + model.free_pages[int(model.free_head):].tolist()) == list(range(POOL))
+    assert model.free_pages.shape == (POOL,) and model.free_head.dtype is model.lengths.dtype is model.free_pages.dtype is torch.int32
+
+
+def test_pages_of_retired_requests_are_used_again(monkeypatch):
+    # a loop that takes several times the pool: seats are vacated at random, refusals included, and every request's outputs are those of a model that has had no other
+    Library(monkeypatch)
+    g = np.random.default_rng(3)
+    model, alone, taken, refused = build(), [build(n_requests=1) for _ in range(3)], 0, 0
+    for n in range(120):
+        fresh = g.integers(0, 4, 3)
+        before, x = model.lengths.clone(), tokens(int(fresh.sum()), n)
+        out, tables = model.step(x, i32(fresh.tolist()))
+        pages_are_whole(model)
+        for b in range(3):
+            grown = int(model.lengths[b] - before[b])
+            assert grown in (0, fresh[b])
+            refused += grown < fresh[b]
+            if grown:
+                rows = tables.request == b
+                want, _ = alone[b].step(x[rows], i32([grown]))
+                assert torch.equal(out[rows], want)
+        done = torch.tensor(g.random(3) < 0.2)
+        gone = [-(-int(v) // P) for v in model.lengths[done]]
+        head = int(model.free_head)
+        model.retire(done)
+        taken += sum(gone)
+        assert int(model.free_head) == head - sum(gone) and (model.lengths[done] == 0).all() and (model.block_table[done] == -1).all()
+        pages_are_whole(model)
+        for b in range(3):
+            if done[b]:
+                alone[b] = build(n_requests=1)
+    assert taken > 3 * POOL and refused > 3
+    model.retire(torch.ones(3, dtype=torch.bool))
+    assert model.free_head.tolist() == [0] and model.lengths.tolist() == [0, 0, 0]
+    pages_are_whole(model)
+
+
+def test_retire_leaves_the_tables_of_the_last_step_and_checks_its_argument(monkeypatch):
+    Library(monkeypatch)
+    model = build()
+    _, tables = model.step(tokens(9, 0), i32([4, 5, 0]))
+    model.retire(torch.tensor([True, False, True]))
+    assert tables.seq_len.tolist() == [4, 5, 0] and tables.free_head.tolist() == [3] and model.lengths.tolist() == [0, 5, 0] and model.free_head.tolist() == [2]
+    for bad in (torch.tensor([1, 0, 1]), torch.tensor([True, False])):
+        with pytest.raises((TypeError, ValueError), match="seats"):
+            model.retire(bad)
+    model.retire(torch.zeros(3, dtype=torch.bool))
+    assert model.lengths.tolist() == [0, 5, 0] and model.free_head.tolist() == [2]
+    _, tables = model.step(tokens(5, 1), i32([4, 1, 0]))
+    assert tables.seq_len.tolist() == [4, 6, 0] and tables.request.tolist() == [0, 0, 0, 0, 1]
+    pages_are_whole(model)
