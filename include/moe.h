@@ -420,6 +420,9 @@ int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t 
  *   natural logarithm of the sum of exponentials; workspace: device, 256-byte aligned, moe_attn_workspace_bytes.  Its first
  *   MOE_ATTN_COUNTER_BYTES must be zero before its first use; every call leaves them zero, for any shape and R.  Two calls
  *   that overlap in time need two.
+ * seq_len, table_row and block_table must not change until the call has finished on the device: blocks that saw different lengths leave rows unwritten or joined too
+ * early, and counters that are not zero, so that the first MOE_ATTN_COUNTER_BYTES have to be zeroed before the workspace is used
+ * again.  Such a call stays within its buffers like any other.
  * A row's bits depend on how the rows of its call are split, and so on their lengths; equal calls give equal bits.
  * q, out and the cache 16-byte aligned; R * ceil(max_pages * page_tokens / 16) < 2^30. */
 #define MOE_ATTN_COUNTER_BYTES 16384

@@ -388,7 +388,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         };
         auto row_now = [&](int x) __attribute__((always_inline)) {
             Now w;
-            w.row = min(base + at, a.R - 1);                 // lengths that change during the call spoil its results and nothing else
+            w.row = min(base + at, a.R - 1);                 // lengths that change during the call (which is not allowed) reach no row that is not there
             w.start = start;
             w.tiles = __builtin_amdgcn_readlane(n_rows, at);
             w.len = __builtin_amdgcn_readlane(rows.len, at);
@@ -771,7 +771,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         int last = 0;
         if (w.row >= 0) {
             int run0;
-            const int n = runs_of_row(dealt, w.start, w.tiles, run0);
+            const int n = runs_within(dealt, w.start, w.tiles, a.runs, run0);
             last = atomicAdd(counters + run0, 1) == n - 1;
         }
         s_last[threadIdx.x] = last;
@@ -781,7 +781,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         if (!s_last[which]) continue;
         const Split w = s_shared[which];
         int run0;
-        const int n = runs_of_row(dealt, w.start, w.tiles, run0);
+        const int n = runs_within(dealt, w.start, w.tiles, a.runs, run0);
         const float* const chain = a.parts + ((size_t)hx * a.runs + run0) * 2 * part_room;     // part k: the second slot of run0, the first of the others
         auto part_of = [&](int k) __attribute__((always_inline)) { return chain + (k ? (size_t)k * 2 : 1) * part_room; };
         // A thread has four values of every part, or of every second, third, .. where there are threads enough; many are loaded at a

@@ -38,5 +38,16 @@ MOE_HD int runs_of_row(const Runs& d, int start, int tiles, int& run0) {
     run0 = (start + d.near) / d.share;
     return (start + tiles - d.near - 1) / d.share - run0 + 1;
 }
+// The same, for the counters and partial results of `runs` blocks that the row is joined through.  Rows of the split are as they are above; a
+// row whose length was changed while the call runs is cut to them, so that it reaches none but these.
+MOE_HD int runs_within(const Runs& d, int start, int tiles, int runs, int& run0) {
+    const int all = d.share * runs;              // no less than there are tiles
+    if (start > all - 1) start = all - 1;
+    if (tiles > all - start) tiles = all - start;
+    int n = runs_of_row(d, start, tiles, run0);
+    if (run0 > runs - 1) run0 = runs - 1;
+    if (n > runs - run0) n = runs - run0;
+    return n < 1 ? 1 : n;
+}
 
 }  // namespace moe
