@@ -340,12 +340,12 @@ __global__ __launch_bounds__(WAVES * 64) void qk_norm_rope_kernel(const RopeArgs
                     v = v * r * load4<false>(gamma + o1);
                 }
             }
-            if (!is_v) {
+            if (!is_v && turns) {                            // 1 and 0 for sine and cosine would not leave the neighbour of an infinite value alone
                 const f32x4 f = u, g = v;
                 if (PAIRS) {
                     u = f32x4{f.x * c.x - f.y * s.x, f.y * c.x + f.x * s.x, f.z * c.y - f.w * s.y, f.w * c.y + f.z * s.y};
                     v = f32x4{g.x * c.z - g.y * s.z, g.y * c.z + g.x * s.z, g.z * c.w - g.w * s.w, g.w * c.w + g.z * s.w};
-                } else if (turns) {
+                } else {
                     u = f * c - g * s;
                     v = g * c + f * s;
                 }

@@ -1,10 +1,10 @@
-"""Attention on the GPU where single values decide: weights with all of their bits, infinite values."""
+"""Attention, norm and rotation on the GPU where single values decide: weights with all of their bits, infinite values."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2411_11217_amd as M
-from test_gpu_attention import DT, HALF_STEP, Cache, f64, i32, queries
+from test_gpu_attention import DT, HALF_STEP, Cache, f64, i32, queries, rope_case
 from util import say
 
 pytestmark = pytest.mark.gpu
@@ -143,3 +143,27 @@ def test_attention_gives_the_infinity_of_a_value_over_many_blocks(dtype):
     kv = M.make_kv_shape(8, 2, 128, 16, c.table.shape[1], c.k.shape[0], dtype)
     q = queries(3, kv, dtype, 4, std=0.5)
     compare_infinite(c, kv, q, lens, dtype, [(0, 0, 1, INF), (0, 8999, 2, -INF), (0, 4000, 3, INF), (0, 7000, 3, -INF), (1, 1200, 100, INF), (1, 1201, 101, -INF), (2, 39, 9, INF)])
+
+
+# ---------------------------------------------------------------------------- norm and rotation
+
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("T", [6, 600])          # eight wavefronts to a row, and four
+@pytest.mark.parametrize("D,rot", [(64, 32), (128, 64), (96, 8), (64, 0), (256, 248)])
+@pytest.mark.parametrize("x_dtype,dtype", [("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32")])
+def test_norm_rope_leaves_elements_behind_rot_dim_to_themselves(D, rot, T, pairs, x_dtype, dtype):
+    kv, x, freq, pos, slots, _, caches = rope_case(T, 4, 2, D, 4, x_dtype, dtype, rot, pairs, False, D + rot)
+    bad = [(1, 0, rot + 3, INF), (1, 0, rot + 4, -0.0), (2, 1, D - 1, -INF), (3, 3, rot, float("nan")), (0, 4, rot + 2, -INF), (T - 1, 5, rot + 5, INF), (T - 1, 2, rot + 1, INF), (T - 1, 2, rot + 6, -INF)]
+    for t, h, d, value in bad:
+        x[t, h * D + d] = value
+    dev = [c.cuda() for c in caches]
+    q = M.moe_qk_norm_rope(kv, x.cuda(), freq.cuda(), pos.cuda(), slots.cuda(), *dev, pairs=pairs)
+    torch.cuda.synchronize()
+    s = slots.long()
+    k = dev[0].cpu()[s // 4, :, s % 4]
+    heads = x.view(T, 8, D)[..., rot:].to(DT[dtype])
+    for got, want in ((q.cpu()[..., rot:], heads[:, :4]), (k[..., rot:], heads[:, 4:6])):
+        nan = want.isnan()
+        assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan], want[~nan]) and torch.equal(torch.signbit(got[~nan]), torch.signbit(want[~nan]))
+    if rot:
+        assert q[..., :rot].isfinite().all() and k[..., :rot].isfinite().all()
