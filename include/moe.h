@@ -390,6 +390,7 @@ int moe_kv_validate(const moe_kv_shape* s);
  *   seq_len: device int32[B], cached + fresh (cached, at least 0, if refused); row_start: device int32[B + 1]; positions,
  *   slots, request: device int32[T], the token's position, slot and request (0, -1, -1 for rows behind the last request's;
  *   slot -1 for refused requests and pages outside the pool); free_head_out: device int32[1].
+ * Without requests and rows (B = T = 0) free_head_out is free_head and row_start[0] is 0, or, where one of these three is NULL, nothing is done.
  * B <= MOE_MAX_REQUESTS.  The outputs must not overlap the inputs: a caller keeps two sets of lengths and heads and takes
  * them in turn. */
 int moe_kv_assign(const moe_kv_shape* s, int32_t B, int32_t T, const int32_t* cached, const int32_t* fresh,

@@ -390,7 +390,7 @@ int moe_kv_assign(const moe_kv_shape* s, int32_t B, int32_t T, const int32_t* ca
     int rc = validate_kv(s);
     if (rc != MOE_OK) return rc;
     if (B < 0 || B > MOE_MAX_REQUESTS || T < 0 || T >= (int32_t)kManyRows || n_free < 0) return MOE_ERR_INVALID_ARG;
-    if (B == 0 && T == 0) return MOE_OK;
+    if (B == 0 && T == 0 && (!free_head || !free_head_out || !row_start)) return MOE_OK;         // nothing to hand on
     if (!free_head || !free_head_out || !row_start || (n_free > 0 && !free_pages)) return MOE_ERR_INVALID_ARG;
     if (B > 0 && (!cached || !fresh || !block_table || !seq_len)) return MOE_ERR_INVALID_ARG;
     if (T > 0 && (!positions || !slots || !request)) return MOE_ERR_INVALID_ARG;
