@@ -824,6 +824,6 @@ def moe_attn_decode(kv: KvShape, q, seq_len, block_table, k_cache, v_cache, scal
             workspace = AttnWorkspace(kv, R, q.device) if workspace is None else workspace
     po = _dev(out, dt, shape, "out")
     ple = None if lse is None else _dev(lse, torch.float32, shape[:2], "lse")
-    _check(_lib().moe_attn_decode(ref, R, pq, pl, pr, pt, table_rows, pk, pv, int(window), head_dim ** -0.5 if scale is None else scale, po, ple,
+    _check(_lib().moe_attn_decode(ref, R, pq, pl, pr, pt, table_rows, pk, pv, max(-1, min(int(window), 2 ** 31 - 1)), head_dim ** -0.5 if scale is None else scale, po, ple,
                                   workspace.buf.data_ptr(), workspace.buf.numel(), ps, _stream(stream)), "moe_attn_decode")
     return out, lse

@@ -3,6 +3,7 @@ own, and what reaches the library is what the handle of the call says."""
 import copy
 import ctypes
 import pickle
+import types
 
 import pytest
 import torch
@@ -98,3 +99,18 @@ def test_the_current_device_is_asked_for_by_its_public_name(monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 5, raising=False)
     assert B._stream(None) == 1003 and asked == ["device"]
     assert B._stream(77) == 77
+
+
+# ---------------------------------------------------------------------------- whole numbers
+
+@pytest.mark.parametrize("window,told_window", [(0, 0), (5, 5), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 32, 2 ** 31 - 1), (2 ** 32 + 5, 2 ** 31 - 1),
+                                                (2 ** 63 - 1, 2 ** 31 - 1), (-1, -1), (-2 ** 32, -1), (-2 ** 33 + 1, -1)])
+def test_a_window_beyond_32_bits_is_not_cut_to_its_low_bits(window, told_window, monkeypatch):
+    # longer than any row is all of it, and what is negative stays refused
+    lib = Recorder(monkeypatch)
+    lib.moe_attn_decode = lambda *args: lib.calls.append(args) or 0
+    kv = M.make_kv_shape(2, 1, 32, 16, 8, 100, "bf16")
+    q, cache = torch.zeros((3, 2, 32), dtype=torch.bfloat16), torch.zeros(kv.cache_shape, dtype=torch.bfloat16)
+    workspace = types.SimpleNamespace(buf=torch.zeros(16))
+    B.moe_attn_decode(kv, q, torch.zeros(3, dtype=torch.int32), torch.zeros((3, 8), dtype=torch.int32), cache, cache, window=window, out=q.clone(), workspace=workspace)
+    assert ctypes.c_int32(lib.calls[-1][9]).value == told_window
