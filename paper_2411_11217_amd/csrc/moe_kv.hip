@@ -375,8 +375,19 @@ int launch_rope(const RopeArgs& a, bool pairs, hipStream_t st) {
 }
 
 template <class In, class Out>
-int launch_rope(const RopeArgs& a, bool pairs, hipStream_t st) {
-    return a.T <= kFewRows ? launch_rope<In, Out, 8>(a, pairs, st) : launch_rope<In, Out, 4>(a, pairs, st);
+int launch_rope(const RopeArgs& all, bool pairs, hipStream_t st) {
+    constexpr int kRows = 1 << 23;                           // of a launch: a grid has less than 2^32 threads
+    for (int t0 = 0; t0 < all.T; t0 += std::min(kRows, all.T - t0)) {
+        RopeArgs a = all;
+        a.T = std::min(kRows, all.T - t0);
+        a.qkv = (const In*)all.qkv + t0 * all.row_elements;
+        a.positions += t0;
+        a.slots += t0;
+        a.q = (Out*)all.q + (int64_t)t0 * all.n_q * all.D;
+        const int rc = a.T <= kFewRows ? launch_rope<In, Out, 8>(a, pairs, st) : launch_rope<In, Out, 4>(a, pairs, st);
+        if (rc != MOE_OK) return rc;
+    }
+    return MOE_OK;
 }
 
 }  // namespace
