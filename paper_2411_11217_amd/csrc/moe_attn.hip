@@ -92,18 +92,20 @@ __device__ __forceinline__ int tiles_of(const Row& w) {
 }
 
 // Rows of prompts.  `pack` rows in a row (16 / heads, from a multiple of `pack` on) that see tokens of one request, up to 8 heads each,
-// share the 16 columns of the MFMA: their tiles are read once instead of once per row.  They do where that is no more tiles than
-// the rows one by one have.  A tile that all of them see whole takes one pass.  In any other the scores are masked column
-// by column, and the second product is made once for each row, with the tokens that this row does not see taken out and the other
-// columns left as they were: a later token's infinity would not be stopped by a weight of 0.
+// share the 16 columns of the MFMA: their tiles are read once instead of once per row.  A tile that all of them see whole takes one
+// pass.  In any other the scores are masked column by column, and the second product is made once for each row, with the tokens that
+// this row does not see taken out and the other columns left as they were: a later token's infinity would not be stopped by a
+// weight of 0.  Where that costs more than it saves (shared_tiles) the rows stay by themselves.
 struct Group {
     int lo, hi, sum;                             // tokens that some row sees; tiles of the rows one by one
+    int clear_lo, clear_hi;                      // tokens that all rows see
     bool one;                                    // a full group, tokens everywhere, one request
 };
 template <int TILE>
-__device__ __forceinline__ int joint_tiles(const Group& g) {      // 0: they do not share
+__device__ __forceinline__ int joint_tiles(const Group& g, int pack) {      // 0: they do not share
     const int n = (int)(((uint32_t)g.hi + TILE - 1) / TILE) - g.lo / TILE;
-    return g.one && n <= g.sum ? n : 0;
+    const int whole = max(0, g.clear_hi / TILE - (int)(((uint32_t)g.clear_lo + TILE - 1) / TILE));
+    return g.one ? shared_tiles(n, whole, pack, g.sum) : 0;
 }
 
 // Sum over the lanes before this one, and over all of them, by data-parallel moves.
@@ -283,27 +285,24 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         if constexpr (PACKED) {
             const int lead = lane - lane % a.pack;
             const uint64_t fit = __ballot(live && own.len > 0 && own.table == __shfl(own.table, lead, 64)), all = ((1ull << a.pack) - 1) << lead;
-            Group grp{own.first, own.len, 0, live && (fit & all) == all};
-            clear_lo = own.first;
-            clear_hi = own.len;
+            Group grp{own.first, own.len, 0, own.first, own.len, live && (fit & all) == all};
             for (int j = 0; j < a.pack; ++j) {
                 const int len = __shfl(own.len, lead + j, 64), first = __shfl(own.first, lead + j, 64);
                 grp.sum += __shfl(n_rows, lead + j, 64);
                 grp.lo = min(grp.lo, first);
                 grp.hi = max(grp.hi, len);
-                clear_lo = max(clear_lo, first);
-                clear_hi = min(clear_hi, len);
+                grp.clear_lo = max(grp.clear_lo, first);
+                grp.clear_hi = min(grp.clear_hi, len);
             }
-            const int shared = joint_tiles<TILE>(grp);
+            const int shared = joint_tiles<TILE>(grp, a.pack);
             joint = shared > 0;
             if (joint) {
                 n_rows = lane == lead ? shared : 0;
                 rows.first = grp.lo;
                 rows.len = grp.hi;
-            } else {
-                clear_lo = own.first;
-                clear_hi = own.len;
             }
+            clear_lo = joint ? grp.clear_lo : own.first;
+            clear_hi = joint ? grp.clear_hi : own.len;
         }
         ahead = wave_sum_before(n_rows, in_rows);
     };
@@ -311,7 +310,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         if constexpr (!PACKED) {
             return tiles_of<TILE>(row_of(a, i, flags));
         } else {
-            Group grp{0x7fffffff, 0, 0, i + a.pack <= a.R};
+            Group grp{0x7fffffff, 0, 0, 0, 0x7fffffff, i + a.pack <= a.R};
             int table = 0;
             for (int j = 0; j < a.pack && i + j < a.R; ++j) {
                 const Row w = row_of(a, i + j, flags);
@@ -319,9 +318,11 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
                 grp.one = grp.one && w.len > 0 && w.table == table;
                 grp.lo = min(grp.lo, w.first);
                 grp.hi = max(grp.hi, w.len);
+                grp.clear_lo = max(grp.clear_lo, w.first);
+                grp.clear_hi = min(grp.clear_hi, w.len);
                 grp.sum += tiles_of<TILE>(w);
             }
-            const int shared = joint_tiles<TILE>(grp);
+            const int shared = joint_tiles<TILE>(grp, a.pack);
             return shared > 0 ? shared : grp.sum;
         }
     };

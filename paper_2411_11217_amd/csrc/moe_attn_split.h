@@ -49,5 +49,11 @@ MOE_HD int runs_within(const Runs& d, int start, int tiles, int runs, int& run0)
     if (n > runs - run0) n = runs - run0;
     return n < 1 ? 1 : n;
 }
+// The tiles that `pack` rows of one request read together, or 0 where they are better read one by one, `sum` tiles: n tiles, `whole` of
+// them seen whole by all rows; any other takes `pack` second products, each about a quarter of what a tile costs that is read once more from the L2.
+// us together / one by one, 16 / 16 heads of 128, 20 groups of 16 rows with 1, 2, 3, 5, 8, 15 of 4000 tokens and the others of 10: 255 / 137, 253 / 165,
+// 254 / 279, 254 / 486, 255 / 714, 281 / 1163 (the rule: one by one up to 3); 32 / 8 heads, 100 groups of 4 rows with 1, 2, 3 of 4000: 315 / 308, 304 / 574, 309 / 841
+// (one by one with 1); rows 16 tokens apart with a window of 32, 16 / 16 heads: 67 / 28, one after another with a window of 10: 39 / 50.
+MOE_HD int shared_tiles(int n, int whole, int pack, int sum) { return n + (n - whole) * pack / 4 <= sum ? n : 0; }
 
 }  // namespace moe

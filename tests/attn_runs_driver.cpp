@@ -46,6 +46,12 @@ int main() {
                     const int m = moe::runs_within(moe::deal_tiles(total, runs), start, t, runs, run0);
                     if (m < 1 || run0 < 0 || run0 + m > runs) fail("outside the workspace", run0, m, runs, start);
                 }
+    // rows of one request that are read together: where that is less work, not where it is only no more tiles
+    const struct { int n, whole, pack, sum, want; } groups[] = {
+        {125, 125, 4, 500, 125}, {125, 1, 4, 376, 125}, {125, 0, 4, 128, 0}, {16, 0, 16, 16, 0}, {16, 0, 16, 79, 0}, {16, 0, 16, 80, 16}, {1, 0, 16, 16, 1}, {1, 0, 2, 2, 1},
+        {2, 1, 3, 5, 2}, {9, 9, 2, 8, 0}, {1 << 26, 0, 16, (1 << 30) - 1, 1 << 26}, {1 << 26, 0, 16, 1 << 26, 0}};
+    for (const auto& c : groups)
+        if (moe::shared_tiles(c.n, c.whole, c.pack, c.sum) != c.want) fail("rows together", c.n, c.whole, c.pack, c.sum);
     if (!outside) fail("no row here leaves the workspace by itself", 0, 0, 0, 0);
     std::printf("all ok\n");
 }

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2411_11217_amd as M
-from test_gpu_attention import i32, new_status
+from test_gpu_attention import Cache, attend_and_compare, i32, new_status, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,23 @@ def test_norm_rope_of_more_rows_than_a_grid_has_threads_for():
     want = M.moe_qk_norm_rope(kv, x[at].contiguous(), freq, rows[at].contiguous(), torch.full((7,), -1, dtype=torch.int32, device="cuda"), k, v)
     torch.cuda.synchronize()
     assert torch.equal(q[at], want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_q,n_kv", [(1, 1), (2, 1), (3, 1), (8, 2), (5, 1), (8, 1)])
+def test_rows_of_one_request_on_both_sides_of_sharing(n_q, n_kv, dtype):
+    # groups whose rows share and groups whose rows do not, in turn: far apart under a window, a few long rows among short ones, all long
+    lens = [900, 260]
+    c = Cache(lens, n_kv, 64, 16, dtype, n_q)
+    kv = M.make_kv_shape(n_q, n_kv, 64, 16, c.table.shape[1], c.k.shape[0], dtype)
+    pack = 16 // (n_q // n_kv)
+    seq, rows = [], []
+    for n in range(45):
+        long = n % (pack + 1)                              # of the group's rows
+        seq += [10 + (7 * n + i) % 20 if i >= long else 850 - 13 * i for i in range(pack)] if n % 3 else [16 * (i + n % 5) + 3 for i in range(pack)]
+        rows += [n % 2 if n % 3 == 0 else 0] * pack
+    seq = [min(s, lens[b]) for s, b in zip(seq, rows)]
+    q = queries(len(seq), kv, dtype, n_q + 1)
+    for n in {len(seq), 64, 3 * pack, 61}:
+        for window in (0, 24, 300):
+            attend_and_compare(c, kv, q[:n], seq[:n], dtype, window=window, table_row=rows[:n], rows=range(0, n, 1 if n < 100 else 5), what=f"{n_q}/{n_kv} {dtype} {n} rows, window {window}")
