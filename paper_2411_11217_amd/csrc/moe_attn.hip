@@ -99,7 +99,16 @@ __device__ __forceinline__ int tiles_of(const Row& w) {
 struct Group {
     int lo, hi, sum;                             // tokens that some row sees; tiles of the rows one by one
     int clear_lo, clear_hi;                      // tokens that all rows see
-    bool one;                                    // a full group, tokens everywhere, one request
+    bool one;                                    // a full group, one request, tokens everywhere, none that no row sees in between
+    // The next row's tokens: they have to touch those of the rows before it, so that no page is followed that no row sees.
+    __device__ __forceinline__ void add(int first, int len, int tiles) {
+        one = one && first <= hi && len >= lo;
+        lo = min(lo, first);
+        hi = max(hi, len);
+        clear_lo = max(clear_lo, first);
+        clear_hi = min(clear_hi, len);
+        sum += tiles;
+    }
 };
 template <int TILE>
 __device__ __forceinline__ int joint_tiles(const Group& g, int pack) {      // 0: they do not share
@@ -285,15 +294,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         if constexpr (PACKED) {
             const int lead = lane - lane % a.pack;
             const uint64_t fit = __ballot(live && own.len > 0 && own.table == __shfl(own.table, lead, 64)), all = ((1ull << a.pack) - 1) << lead;
-            Group grp{own.first, own.len, 0, own.first, own.len, live && (fit & all) == all};
-            for (int j = 0; j < a.pack; ++j) {
-                const int len = __shfl(own.len, lead + j, 64), first = __shfl(own.first, lead + j, 64);
-                grp.sum += __shfl(n_rows, lead + j, 64);
-                grp.lo = min(grp.lo, first);
-                grp.hi = max(grp.hi, len);
-                grp.clear_lo = max(grp.clear_lo, first);
-                grp.clear_hi = min(grp.clear_hi, len);
-            }
+            const int first = __shfl(own.first, lead, 64), len = __shfl(own.len, lead, 64);
+            Group grp{first, len, __shfl(n_rows, lead, 64), first, len, live && (fit & all) == all};
+            for (int j = 1; j < a.pack; ++j) grp.add(__shfl(own.first, lead + j, 64), __shfl(own.len, lead + j, 64), __shfl(n_rows, lead + j, 64));
             const int shared = joint_tiles<TILE>(grp, a.pack);
             joint = shared > 0;
             if (joint) {
@@ -310,17 +313,12 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 2 : 1) void attn_kernel(const 
         if constexpr (!PACKED) {
             return tiles_of<TILE>(row_of(a, i, flags));
         } else {
-            Group grp{0x7fffffff, 0, 0, 0, 0x7fffffff, i + a.pack <= a.R};
-            int table = 0;
-            for (int j = 0; j < a.pack && i + j < a.R; ++j) {
+            const Row lead = row_of(a, i, flags);
+            Group grp{lead.first, lead.len, tiles_of<TILE>(lead), lead.first, lead.len, i + a.pack <= a.R && lead.len > 0};
+            for (int j = 1; j < a.pack && i + j < a.R; ++j) {
                 const Row w = row_of(a, i + j, flags);
-                if (j == 0) table = w.table;
-                grp.one = grp.one && w.len > 0 && w.table == table;
-                grp.lo = min(grp.lo, w.first);
-                grp.hi = max(grp.hi, w.len);
-                grp.clear_lo = max(grp.clear_lo, w.first);
-                grp.clear_hi = min(grp.clear_hi, w.len);
-                grp.sum += tiles_of<TILE>(w);
+                grp.one = grp.one && w.len > 0 && w.table == lead.table;
+                grp.add(w.first, w.len, tiles_of<TILE>(w));
             }
             const int shared = joint_tiles<TILE>(grp, a.pack);
             return shared > 0 ? shared : grp.sum;

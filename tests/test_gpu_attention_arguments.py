@@ -58,3 +58,14 @@ def test_rows_of_one_request_on_both_sides_of_sharing(n_q, n_kv, dtype):
     for n in {len(seq), 64, 3 * pack, 61}:
         for window in (0, 24, 300):
             attend_and_compare(c, kv, q[:n], seq[:n], dtype, window=window, table_row=rows[:n], rows=range(0, n, 1 if n < 100 else 5), what=f"{n_q}/{n_kv} {dtype} {n} rows, window {window}")
+
+
+@pytest.mark.parametrize("n_q,n_kv,lens", [(4, 1, [300, 300, 300, 640]), (4, 1, [640, 300, 300, 300]), (2, 1, [300] * 7 + [640]), (4, 1, [300, 300, 300, 640] * 40)])
+def test_pages_between_the_windows_of_rows_that_share_are_not_followed(n_q, n_kv, lens):
+    # rows of one request under a window: what no row sees may be gone from the block table
+    c = Cache([640], n_kv, 64, 16, "bf16", 2)
+    kv = M.make_kv_shape(n_q, n_kv, 64, 16, c.table.shape[1], c.k.shape[0], "bf16")
+    q, rows = queries(len(lens), kv, "bf16", 3), [0] * len(lens)
+    for gone in (-1, 2 ** 31 - 1):
+        c.table[0, 19:21] = gone                           # tokens 304 to 335; the rows see 0 to 299 and 340 to 639
+        attend_and_compare(c, kv, q, lens, "bf16", window=300, table_row=rows)
