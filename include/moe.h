@@ -406,7 +406,7 @@ int moe_kv_assign(const moe_kv_shape* s, int32_t B, int32_t T, const int32_t* ca
  *   follows, as moe_pre_attention's qkv; row_elements * element size a multiple of 16; q_gamma, k_gamma: device
  *   float[head_dim]; inv_freq: device double[rot_dim / 2], radians per position; rot_dim a multiple of 8, 0 .. head_dim;
  *   positions, slots: device int32[T]; q: device dtype[T][n_q][head_dim].  Two rows with one slot: either may be left.
- * qkv, q and the cache 16-byte aligned. */
+ * qkv, q, q_gamma, k_gamma and the cache 16-byte aligned. */
 int moe_qk_norm_rope(const moe_kv_shape* s, int32_t T, const void* qkv, int32_t qkv_dtype, int64_t row_elements,
                      const float* q_gamma, const float* k_gamma, float eps, const double* inv_freq, int32_t rot_dim,
                      int32_t pairs, const int32_t* positions, const int32_t* slots, void* q, void* k_cache, void* v_cache,

@@ -84,7 +84,7 @@ def attend(q, k, v, scale, split_p):
     """q [G, D], k and v [n, D] (exact in double).  -> (out [G, D], lse [G], bound [G, D], lse_bound [G]).  The bound: a score is a chain
     of D products and sums, off by (D + 2) u sum |q k| scale, and with the running maximum and the exponent's argument by 6 u (|s| + |max|);
     twice that is the relative error of a weight against the sum of all weights, each of them off by another 4 u, the sums by u per
-    addition in a chain (at most n / 4 + 32), and where the weights are split in two bf16 parts (split_p) by 2^-15."""
+    addition in a chain (at most n / 4 + 32), and with split_p by 2^-15 more, as weights that are held in 16 bits."""
     n, D = k.shape
     if n == 0:
         return np.zeros_like(q), np.full(len(q), -np.inf), np.zeros_like(q), np.zeros(len(q))

@@ -22,12 +22,13 @@
 // nothing is rounded.  A part of 0 would make 0 * infinity of an infinite value, so no part of a weight that is not 0 is 0: the
 // first is the largest number of 8 bits below the weight, the second that below what is left, the third the rest (1 to 256
 // units of the weight's last place).  f32: 16x16x4 MFMAs, 16 tokens, nothing is rounded either.
-//   The matrix cores are busy a quarter of the time (131001 tokens, 48 heads), so the columns that fewer than 16 heads leave empty cost nothing.
+//   The matrix cores are busy a third of the time (131001 tokens, 48 heads), so the columns that fewer than 16 heads leave empty cost nothing.
 //
 // us in a graph, and what of the bytes that is (a load-only kernel reads 6.2 TB/s here, 7.1 with the non-temporal hint; an empty launch takes 2):
-// three float32 requests of up to 130 tokens 4.8; 36 requests of 60 to 700 tokens, 32 / 8 heads of 128, 15 (2.4 TB/s); 900 rows of six
-// prompts 26; one request of 131001 tokens, 48 / 8 heads, 95 (5.7 TB/s); a window of 1000 tokens over 61
-// requests, 20 / 20 heads of 96, 76 (5.2 TB/s); 256 requests of 500 to 5000 tokens, 32 / 8 heads, 325 (6.3 TB/s).
+// three float32 requests of up to 130 tokens 4.9; 36 requests of 60 to 700 tokens, 32 / 8 heads of 128, 15.7 (2.4 TB/s); 830 rows of six
+// prompts 27; one request of 131001 tokens, 48 / 8 heads, 95 (5.6 TB/s); a window of 1000 tokens over 61
+// requests, 20 / 20 heads of 96, 78 (5.1 TB/s); 256 requests of 500 to 5000 tokens, 32 / 8 heads, 322 to 334 (6.4 to 6.1 TB/s); in
+// float32 128 such requests 322 (6.3 TB/s), one of 131001 tokens, 48 / 8 heads, 183 (5.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -865,7 +866,7 @@ Plan plan_of(const moe_kv_shape& s, int32_t R, bool prompts) {
     const int64_t heads_x = (int64_t)s.n_kv * p.head_tiles;
     const int64_t tiles = R * (((int64_t)s.max_pages * s.page_tokens + tile - 1) / tile);
     // Two for each of the 256 compute units, all of them at once.  us with one, two, four, in an earlier build: 256 requests 365 / 347 / 377,
-    // 36 requests 20 / 20 / 24, one request of 131001 tokens 102 / 102 / 126, 900 prompt rows 69 / 49 / 58.
+    // 36 requests 20 / 20 / 24, one request of 131001 tokens 102 / 102 / 126, 830 prompt rows 69 / 49 / 58.
     constexpr int kBlocks = 512;
     p.runs = (int)std::max<int64_t>(1, std::min<int64_t>({kBlocks / heads_x, (tiles + kLeastTiles - 1) / kLeastTiles}));
     p.parts_bytes = (size_t)heads_x * p.runs * 2 * far_floats(s.head_dim, H) * 4;
@@ -891,9 +892,10 @@ int launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
 
 // Rows with a table row of their own and at most 16 query heads to a key/value head read every key and value once: those loads carry
 // the non-temporal hint (us without / with: 256 requests 374 / 347, one request of 131001 tokens 114 / 102).  Rows that name their table row
-// may be a prompt's, and share columns where there is room for two.  us, each row by itself / sharing, 32 / 8 heads of 128: 900 rows of six
-// prompts 37 / 26, 18600 rows of 128 prompts 724 / 347, a prompt of 4000 tokens 1492 / 500, 2200 rows of 200 prompts of 5 to 20 tokens 31 /
-// 32; 20 / 20 heads of 96, three prompts of up to 418 tokens 54 / 36; float32, 8 / 2 heads 28.7 / 28.2.
+// may be a prompt's, and share columns where there is room for two.  us, each row by itself / sharing, 32 / 8 heads of 128: 830 rows of six
+// prompts 43 / 28, 18636 rows of 128 prompts 767 / 359, a prompt of 4000 tokens 1849 / 564, 2468 rows of 200 prompts of 5 to 20 tokens 38 /
+// 35; 20 / 20 heads of 96, prompts of 418, 200 and 60 tokens 91 / 43; float32, 8 / 2 heads, 830 rows 36 / 29, 32 / 8 heads, a prompt of 4000 tokens 5665 / 1627.
+// Single tokens that name their table row pay for that: 256 requests of 500 to 5000 tokens 370 where they take 321 without, 36 requests 17.4 / 15.7.
 template <class Elem, int D>
 int launch(const AttnArgs& a, const Plan& p, hipStream_t st) {
     if (p.pack > 1) return launch<Elem, D, false, true>(a, p, st);

@@ -15,7 +15,7 @@ namespace moe {
 // tokens 16 either way.)
 constexpr int kLeastTiles = 4;
 // How many tiles the end of a block may move to meet the end of a row, so that the row is not shared with another block.  (us
-// with 0 / 2 / 4 / 8: 36 requests of 60 to 700 tokens 19.8 / 17.6 / 16.0 / 16.2, 900 prompt rows 40 / 40 / 37 / 37, long requests the same.)
+// with 0 / 2 / 4 / 8: 36 requests of 60 to 700 tokens 19.8 / 17.6 / 16.0 / 16.2, 830 prompt rows 40 / 40 / 37 / 37, long requests the same.)
 constexpr int kNearTiles = 4;
 
 // Block w has the tiles from run_end(w * share) to run_end((w + 1) * share).

@@ -196,7 +196,8 @@ __global__ __launch_bounds__(THREADS) void assign_kernel(const AssignArgs a) {
 
 template <int THREADS, int PER, int ROWS>
 int launch_assign(const AssignArgs& a, hipStream_t st) {
-    // a block for as many rows as its threads take at once; beyond two blocks of 256 threads per compute unit they stride
+    // a block for as many rows as its threads take at once; beyond 2^17 threads (512 blocks of 256, 128 of 1024: half of the compute
+    // units) they stride
     const int blocks = (int)std::min<int64_t>(std::max<int64_t>(((int64_t)a.T + ROWS * THREADS - 1) / (ROWS * THREADS), 1), 2 * 256 * 256 / THREADS);
     hipLaunchKernelGGL((assign_kernel<THREADS, PER, ROWS>), dim3(blocks), dim3(THREADS), (size_t)a.B * 8, st, a);
     MOE_HIP_TRY(hipGetLastError());
@@ -219,7 +220,8 @@ int launch_assign(const AssignArgs& a, hipStream_t st) {
 // rotation needs no other lane; elsewhere they are neighbours.  rot_dim is a multiple of 8, so no lane has both kinds.
 // The angle is formed in 64 bits as a number of turns, whose whole part falls away exactly: at position 10^6 a float
 // product would be off by 0.03 radians.  Every wavefront forms the four angles of its lanes once for all of its heads.  9857 rows of 48 + 2 * 8 heads
-// of 128, 484 MB: 83 us; a large copy moves 4.96 TB/s here.  256 rows of 32 + 2 * 8 heads 4.4 us, of which 2.9 are the launch.
+// of 128, 484 MB: 83 us, where a kernel that only copies such rows, with the same hints, takes 80.5; float32 to float32,
+// 646 MB, 115 and 108.5.  256 rows of 32 + 2 * 8 heads 4.4 us, of which 2.9 are the launch.
 constexpr int kFewRows = 512;
 
 struct RopeArgs {

@@ -1,5 +1,5 @@
 """Decode with the key-value cache in device memory: a stack of attention + MoE layers of one shape, stepped over the fresh tokens of a
-batch of requests -- whole prompts, single tokens, or both in one step.
+batch of requests -- whole prompts, single tokens, or both in one step -- with the seats and pages of requests that are done used again.
 
     tables of the step (moe_kv_assign, once)
     for each layer:  residual + norm + QKV projection (moe_pre_attention), norm and rotation into the layer's cache
