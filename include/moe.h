@@ -25,7 +25,7 @@
  *  - dtype is the storage type of x, the router, the expert weights and the
  *    intermediate h; logits, gate weights, expert outputs and y are float.
  *
- * Supported shapes: 1 <= k <= E <= MOE_MAX_EXPERTS, H and F multiples of 128,
+ * Supported shapes: 1 <= k <= E <= MOE_MAX_EXPERTS, H and F multiples of 128 (MOE_DTYPE_I8: of 256, below 2^17),
  * page_bytes a positive multiple of the weight-tile size (moe_tile_bytes).
  */
 #ifndef MOE_H_
@@ -49,7 +49,7 @@ typedef enum moe_status {
     MOE_ERR_HIP = -5                 /* a HIP call failed; see moe_last_hip_error() */
 } moe_status;
 
-enum { MOE_DTYPE_F32 = 0, MOE_DTYPE_BF16 = 1 };
+enum { MOE_DTYPE_F32 = 0, MOE_DTYPE_BF16 = 1, MOE_DTYPE_I8 = 2 };    /* MOE_DTYPE_I8: "the layer in 8-bit integers" below */
 
 typedef struct moe_shape {
     int32_t T;          /* tokens in the micro-batch (mu) */
@@ -71,12 +71,14 @@ int moe_validate_shape(const moe_shape* s);
  *
  * Page format (this library's reading of the paper's weight pages, appendix
  * A.1; the paper fixes neither page size nor content).  The unit is a TILE of
- * 128 output features x 64 reduction elements (16 KiB bf16, 32 KiB f32).
+ * 128 output features x 64 reduction elements (16 KiB bf16, 32 KiB f32), of 8-bit integers 128 x 128 (16 KiB).
  *   f32:  128 rows of 256 bytes; the 16-byte chunk with index c (0..15) of row n
  *         is stored at chunk position (c & 8) | ((c & 7) ^ ((n >> 1) & 7)).
  *   bf16: two half-tiles of 8 KiB, one per 32 reduction elements; half-tile c >> 2
  *         holds, in row n of 64 bytes, chunk c (0..7) of that row at chunk position
  *         (c & 3) ^ ((n >> 2) & 2).
+ *   8-bit integers: as bf16, with 64 reduction elements to a half-tile's row.  The tile counts below are those of bf16; k
+ *         counts in steps of 128.
  * These are the images the GEMM kernels copy straight into LDS (the bf16 kernel
  * consumes 32 reduction elements per pipeline stage).  The LDS has 64 banks of
  * 4 bytes, a 128-bit LDS read executes in four phases of 16 lanes (for the bf16
@@ -177,8 +179,8 @@ int moe_expert_ffn(const moe_shape* s, const void* x_perm, const int32_t* offset
 
 /* a4. Un-permute and combine: y[t] = sum_slot w * out[row_of[t*k+slot]], with
  * w = topk_w[t][slot], or 1 when topk_w == NULL (weight already applied).
- * out: device float[R][H]; y: device float[T][H]. */
-int moe_combine(const moe_shape* s, const float* out, const int32_t* row_of,
+ * out: device float[R][H], with MOE_DTYPE_I8 bf16[R][H]; y: device float[T][H]. */
+int moe_combine(const moe_shape* s, const void* out, const int32_t* row_of,
                 const float* topk_w, float* y, void* stream);
 
 /* a5. The whole layer in one call, on one stream, without host synchronisation.
@@ -301,14 +303,14 @@ typedef struct moe_linear_shape {
     int32_t T;          /* rows (tokens) */
     int32_t K;          /* input features */
     int32_t N;          /* output features */
-    int32_t dtype;      /* MOE_DTYPE_BF16 */
+    int32_t dtype;      /* MOE_DTYPE_BF16, or MOE_DTYPE_I8 (moe_linear_i8) */
     int64_t page_bytes;
 } moe_linear_shape;
 
 #define MOE_LINEAR_WORKSPACE_BYTES 16
 
 int moe_linear_pages_required(const moe_linear_shape* s, int64_t* pages);
-/* Host packer.  W: host bf16[N][K]; page_table: host int32[pages], distinct slots in
+/* Host packer.  W: host dtype[N][K]; page_table: host int32[pages], distinct slots in
  * [0, pool_pages); pages_out: host, pool_pages * page_bytes. */
 int moe_linear_pack(const moe_linear_shape* s, const void* W, const int32_t* page_table, int64_t pool_pages,
                     void* pages_out);
@@ -346,6 +348,74 @@ int moe_pre_attention(const moe_linear_shape* qkv_proj, const float* hidden, con
                       float eps, const int32_t* qkv_table, const void* page_pool, int64_t pool_pages,
                       float* hidden_out, void* x_norm, float* qkv, void* qkv_bf16, void* workspace, size_t workspace_bytes,
                       void* stream);
+
+/* ------------------------------------------------------------------ the layer in 8-bit integers
+ *
+ * The experts' products and the linear maps on 8-bit integers, with a scale for each row of activations (each token) and each output
+ * channel of a weight: half the weight bytes of bf16, and matrix cores that multiply twice as many.  A value is q * scale with q from
+ * -127 to 127; scale = max |row| / 127, at least 2^-126, q = the whole number next to value * (127 / max |row|), ties to even, in float
+ * arithmetic.  A row that holds an infinity or a NaN has the scale NaN and zeros for q, so that what is computed from it is NaN.
+ * A product adds whole numbers, exactly, and multiplies the sum by the scales of its column and its row in float.
+ *
+ * Weights are quantised by their output channels, the rows of W1, W3, W2 and of a linear map's W, with moe_quantize_i8 or by any other
+ * rule (-128 is allowed), and packed by moe_pack_weights and moe_linear_pack with a shape of MOE_DTYPE_I8.  Of the calls above
+ * moe_validate_shape, moe_tile_bytes, moe_pages_required, moe_pack_weights, moe_unpack_weights, moe_page_table_validate, moe_combine,
+ * moe_linear_pages_required and moe_linear_pack take such a shape, all others MOE_DTYPE_F32 or MOE_DTYPE_BF16 alone: router and
+ * permutation take the bf16 shape with otherwise the same fields.
+ * Sizes: H, F and a linear map's K multiples of 256 below 2^17, N a multiple of 128; T * H < 2^32.  A row's bits depend neither on how many
+ * rows its call has nor on what they hold. */
+
+/* Rows in 8 bits.  x: device, float or bf16 (x_dtype) [T][N], row t at x + t * row_elements; x_q: device int8[T][N]; x_scale: device
+ * float[T].  N and row_elements multiples of 4, x aligned to four of its elements, x_q to 4 bytes; no two of them overlap. */
+int moe_quantize_i8(int32_t T, int32_t N, const void* x, int32_t x_dtype, int64_t row_elements, int8_t* x_q, float* x_scale,
+                    void* stream);
+
+/* moe_add_rmsnorm with its rows in 8 bits: s = hidden + delta (hidden may be NULL), written to hidden_out when not NULL;
+ * y = s / sqrt(mean(s^2) + eps) * gamma in float; x_q, x_scale: y in 8 bits; x_out: bf16(y), or NULL.  H a multiple of 4, at most 8192;
+ * arrays of float 16-byte, x_out 8-byte aligned.  hidden_out may be hidden or delta; otherwise no output overlaps anything. */
+int moe_add_rmsnorm_i8(int32_t T, int32_t H, const float* hidden, const float* delta, const float* gamma, float eps,
+                       float* hidden_out, void* x_out, int8_t* x_q, float* x_scale, void* stream);
+
+/* out[t][n] = (sum_k x_q[t][k] W[n][k]) * w_scale[n] * x_scale[t].  x_q: device int8[T][K], 16-byte aligned; x_scale: device float[T];
+ * page_table: device int32[pages] (moe_linear_pages_required); w_scale: device float[N]; out: device float[T][N]; status as for moe_linear. */
+int moe_linear_i8(const moe_linear_shape* s, const int8_t* x_q, const float* x_scale, const int32_t* page_table, const void* page_pool,
+                  int64_t pool_pages, const float* w_scale, float* out, int32_t* status, void* stream);
+
+typedef struct moe_expert_scales {      /* device arrays */
+    const float* w1;    /* [E][F], of the rows of W1 (gate) */
+    const float* w3;    /* [E][F], of W3 (up) */
+    const float* w2;    /* [E][H], of W2 (down) */
+} moe_expert_scales;
+
+/* Grouped SwiGLU expert FFN.  Row r of expert e is x_q[row_src[r] / k] (row_src NULL: x_q[r]) with its scale:
+ *   h[r] = bf16(silu(g) * u), g and u from W1_e and W3_e;  h_q[r], h_scale[r]: h[r] in 8 bits;  out[r] = bf16(row_w[r] * (W2_e h[r])).
+ * x_q: device int8[T][H] with row_src (device int32[R]), else int8[R][H]; x_scale: float[T] or float[R]; h: device bf16[R][F];
+ * h_q: device int8[R][F]; h_scale: device float[R]; out: device bf16[R][H]; row_w: device float[R] or NULL; status as for moe_expert_ffn.
+ * x_q, h, h_q, out and the pool 16-byte aligned; none of what is written overlaps anything else. */
+int moe_expert_ffn_i8(const moe_shape* s, const int8_t* x_q, const float* x_scale, const int32_t* row_src, const int32_t* offsets,
+                      const int32_t* page_table, const void* page_pool, int64_t pool_pages, const moe_expert_scales* scales,
+                      const float* row_w, void* h, int8_t* h_q, float* h_scale, void* out, int32_t* status, void* stream);
+
+/* The whole layer: router on x (device bf16[T][H], Wr bf16), experts on the same rows in 8 bits (x_q, x_scale), combine.  y: device
+ * float[T][H]; workspace: device, 256-byte aligned; its first word is the status word, cleared by the call. */
+int moe_layer_i8_workspace_bytes(const moe_shape* s, size_t* bytes);
+int moe_layer_i8(const moe_shape* s, const void* x, const int8_t* x_q, const float* x_scale, const void* Wr, const float* bias,
+                 const int32_t* page_table, const void* page_pool, int64_t pool_pages, const moe_expert_scales* scales, float* y,
+                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* moe_pre_attention and moe_post_attention in 8 bits.  Pre: hidden_out = hidden + delta, x_q and x_scale its norm in 8 bits,
+ * qkv = the projection (float[T][N]).  Post: attn (device bf16[T][o_proj->K]) in 8 bits, O projection, residual and norm (hidden_mid,
+ * x_moe bf16, and in 8 bits in the workspace), moe_layer_i8.  (As in moe_post_attention an entry of o_table outside the pool is read as
+ * page 0 and not reported.)  workspace: device, 256-byte aligned, the layer's at its start. */
+int moe_pre_attention_i8(const moe_linear_shape* qkv_proj, const float* hidden, const float* delta, const float* norm_gamma, float eps,
+                         const int32_t* qkv_table, const void* page_pool, int64_t pool_pages, const float* qkv_scale, float* hidden_out,
+                         int8_t* x_q, float* x_scale, float* qkv, int32_t* status, void* stream);
+int moe_post_attention_i8_workspace_bytes(const moe_shape* s, const moe_linear_shape* o_proj, size_t* bytes);
+int moe_post_attention_i8(const moe_shape* s, const moe_linear_shape* o_proj, const void* attn, const float* hidden,
+                          const int32_t* o_table, const float* o_scale, const float* norm_gamma, float eps, const void* Wr,
+                          const float* bias, const int32_t* page_table, const void* page_pool, int64_t pool_pages,
+                          const moe_expert_scales* scales, float* hidden_mid, void* x_moe, float* y, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ attention over a paged key-value cache
  *

@@ -20,7 +20,8 @@ from . import build as _build
 
 _i32, _i64, _vp, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
 
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_I8 = 0, 1, 2
+_TORCH_DTYPES = (torch.float32, torch.bfloat16, torch.int8)
 MAX_EXPERTS = 64
 
 
@@ -35,10 +36,25 @@ class MoEShape(ctypes.Structure):
 
     @property
     def torch_dtype(self):
-        return torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float32
+        return _TORCH_DTYPES[self.dtype] if 0 <= self.dtype < 3 else torch.float32
 
     def with_tokens(self, T: int) -> "MoEShape":
         return MoEShape(T, self.H, self.F, self.E, self.k, self.dtype, self.page_bytes)
+
+    def routed(self) -> "MoEShape":
+        """The shape for moe_route and moe_permute beside 8-bit experts: their activations are bf16."""
+        return MoEShape(self.T, self.H, self.F, self.E, self.k, DTYPE_BF16 if self.dtype == DTYPE_I8 else self.dtype, self.page_bytes)
+
+
+class ExpertScales:
+    """Scales of the experts' output channels, device float32: w1 and w3 [E, F], w2 [E, H]."""
+
+    def __init__(self, w1: torch.Tensor, w3: torch.Tensor, w2: torch.Tensor):
+        self.w1, self.w3, self.w2 = w1, w3, w2
+
+    def pointers(self, s: MoEShape):
+        return (_vp * 3)(_dev(self.w1, torch.float32, (s.E, s.F), "scales.w1"), _dev(self.w3, torch.float32, (s.E, s.F), "scales.w3"),
+                         _dev(self.w2, torch.float32, (s.E, s.H), "scales.w2"))
 
 
 class WorkspaceLayout(ctypes.Structure):
@@ -89,6 +105,15 @@ _SIGNATURES = {
     "moe_post_attention_workspace_bytes": (ctypes.c_int, [_vp, _vp]),
     "moe_post_attention": (ctypes.c_int, [_vp] * 6 + [ctypes.c_float] + [_vp] * 4 + [_i64] + [_vp] * 4 + [_sz, _vp]),
     "moe_pre_attention": (ctypes.c_int, [_vp] * 4 + [ctypes.c_float, _vp, _vp, _i64] + [_vp] * 5 + [_sz, _vp]),
+    "moe_quantize_i8": (ctypes.c_int, [_i32, _i32, _vp, _i32, _i64, _vp, _vp, _vp]),
+    "moe_add_rmsnorm_i8": (ctypes.c_int, [_i32, _i32, _vp, _vp, _vp, ctypes.c_float] + [_vp] * 5),
+    "moe_linear_i8": (ctypes.c_int, [_vp] * 5 + [_i64] + [_vp] * 4),
+    "moe_expert_ffn_i8": (ctypes.c_int, [_vp] * 7 + [_i64] + [_vp] * 8),
+    "moe_layer_i8_workspace_bytes": (ctypes.c_int, [_vp, _vp]),
+    "moe_layer_i8": (ctypes.c_int, [_vp] * 8 + [_i64, _vp, _vp, _vp, _sz, _vp]),
+    "moe_pre_attention_i8": (ctypes.c_int, [_vp] * 4 + [ctypes.c_float, _vp, _vp, _i64] + [_vp] * 7),
+    "moe_post_attention_i8_workspace_bytes": (ctypes.c_int, [_vp, _vp, _vp]),
+    "moe_post_attention_i8": (ctypes.c_int, [_vp] * 7 + [ctypes.c_float] + [_vp] * 4 + [_i64] + [_vp] * 5 + [_sz, _vp]),
     "moe_kv_validate": (ctypes.c_int, [_vp]),
     "moe_kv_assign": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _i32] + [_vp] * 10),
     "moe_qk_norm_rope": (ctypes.c_int, [_vp, _i32, _vp, _i32, _i64, _vp, _vp, ctypes.c_float, _vp, _i32, _i32] + [_vp] * 7),
@@ -157,7 +182,7 @@ def _dev(t: Optional[torch.Tensor], dtype, shape, name: str) -> Optional[int]:
 
 
 def make_shape(T, H, F, E, k, dtype, page_bytes) -> MoEShape:
-    code = {"f32": 0, "bf16": 1, torch.float32: 0, torch.bfloat16: 1, 0: 0, 1: 1}[dtype]
+    code = {"f32": 0, "bf16": 1, "i8": 2, torch.float32: 0, torch.bfloat16: 1, torch.int8: 2, 0: 0, 1: 1, 2: 2}[dtype]
     return MoEShape(int(T), int(H), int(F), int(E), int(k), code, int(page_bytes))
 
 
@@ -319,8 +344,8 @@ def moe_expert_ffn(s: MoEShape, x_perm, offsets, page_table, page_pool, row_w=No
 
 
 def moe_combine(s: MoEShape, out, row_of, topk_w=None, stream=None):
-    """-> y float32 [T,H]"""
-    po = _dev(out, torch.float32, (s.R, s.H), "out")
+    """out float32 [R,H], with 8-bit experts bf16 -> y float32 [T,H]"""
+    po = _dev(out, torch.bfloat16 if s.dtype == DTYPE_I8 else torch.float32, (s.R, s.H), "out")
     pr = _dev(row_of, torch.int32, (s.R,), "row_of")
     pw = _dev(topk_w, torch.float32, (s.T, s.k), "topk_w")
     y = torch.empty((s.T, s.H), dtype=torch.float32, device=out.device)
@@ -557,8 +582,9 @@ class LinearShape(ctypes.Structure):
                 ("page_bytes", ctypes.c_int64)]
 
 
-def make_linear_shape(T, K, N, page_bytes) -> LinearShape:
-    return LinearShape(int(T), int(K), int(N), DTYPE_BF16, int(page_bytes))
+def make_linear_shape(T, K, N, page_bytes, dtype="bf16") -> LinearShape:
+    code = {"bf16": 1, "i8": 2, torch.bfloat16: 1, torch.int8: 2, 1: 1, 2: 2}[dtype]
+    return LinearShape(int(T), int(K), int(N), code, int(page_bytes))
 
 
 def linear_pages_required(ls: LinearShape) -> int:
@@ -574,10 +600,10 @@ def _linear_pages_required(*fields):
 
 
 def linear_pack(ls: LinearShape, W: torch.Tensor, page_table: torch.Tensor, pages_out: torch.Tensor):
-    """Writes the pages of W (host bf16 [N,K]) into pages_out (host uint8 [pool_pages, page_bytes]) at the slots
+    """Writes the pages of W (host bf16 or int8 [N,K], by ls.dtype) into pages_out (host uint8 [pool_pages, page_bytes]) at the slots
     page_table (host int32 [pages]) names."""
     n = linear_pages_required(ls)
-    pw = _host(W, torch.bfloat16, (ls.N, ls.K), "W")
+    pw = _host(W, _TORCH_DTYPES[ls.dtype], (ls.N, ls.K), "W")
     pt = _host(page_table, torch.int32, (n,), "page_table")
     pp = _host(pages_out, torch.uint8, (pages_out.shape[0], ls.page_bytes), "pages_out")
     _check(_lib().moe_linear_pack(ctypes.byref(ls), pw, pt, int(pages_out.shape[0]), pp), "moe_linear_pack")
@@ -665,6 +691,190 @@ def moe_pre_attention(qkv_proj: LinearShape, hidden, delta, norm_gamma, eps, qkv
                                     None if qkv16 is None else qkv16.data_ptr(), qkv.data_ptr(), 16, _stream(stream)),
            "moe_pre_attention")
     return hidden_out, x_norm, qkv, qkv16
+
+
+# ----------------------------------------------------------------------------- the layer in 8-bit integers
+
+def _pool(page_pool, page_bytes: int) -> int:
+    pp = _dev(page_pool, torch.uint8, None, "page_pool")
+    if page_pool.dim() != 2 or page_pool.shape[1] != page_bytes:
+        raise ValueError("page_pool: expected uint8 [pool_pages, page_bytes]")
+    return pp
+
+
+def _optional(t, dtype, shape, name):
+    return None if t is None else _dev(t, dtype, shape, name)
+
+
+def moe_quantize_i8(x, x_q: Optional[torch.Tensor] = None, x_scale: Optional[torch.Tensor] = None, stream=None):
+    """x float32 or bf16 [T, N], elements of a row next to each other, N and the rows' distance multiples of 4
+    -> (x_q int8 [T, N], x_scale float32 [T]); x_q * x_scale[:, None] stands for x."""
+    if x.dim() != 2:
+        raise ValueError(f"x: expected two dimensions, got {x.dim()}")
+    T, N = x.shape
+    if not x.is_cuda:
+        raise ValueError("x: must be a CUDA/HIP device tensor")
+    if x.dtype is not torch.float32 and x.dtype is not torch.bfloat16:
+        raise TypeError(f"x: expected torch.float32 or torch.bfloat16, got {x.dtype}")
+    if N > 1 and x.stride(1) != 1:
+        raise ValueError("x: the elements of a row must be next to each other")
+    if x_q is None or x_scale is None:
+        with _on(stream):
+            x_q = torch.empty((T, N), dtype=torch.int8, device=x.device) if x_q is None else x_q
+            x_scale = torch.empty(T, dtype=torch.float32, device=x.device) if x_scale is None else x_scale
+    pq = _dev(x_q, torch.int8, (T, N), "x_q")
+    ps = _dev(x_scale, torch.float32, (T,), "x_scale")
+    _check(_lib().moe_quantize_i8(T, N, x.data_ptr(), DTYPE_F32 if x.dtype is torch.float32 else DTYPE_BF16, x.stride(0) if T > 1 else N, pq, ps, _stream(stream)),
+           "moe_quantize_i8")
+    return x_q, x_scale
+
+
+def moe_add_rmsnorm_i8(hidden, delta, gamma, eps: float, want_hidden: bool = True, want_x: bool = True, stream=None):
+    """-> (hidden + delta float32 or None, normalised rows bf16 or None, the same rows in 8 bits int8 [T, H], their scales float32 [T])"""
+    T, H = delta.shape
+    ph = _optional(hidden, torch.float32, (T, H), "hidden")
+    pd = _dev(delta, torch.float32, (T, H), "delta")
+    pg = _dev(gamma, torch.float32, (H,), "gamma")
+    dev = delta.device
+    with _on(stream):
+        hs = torch.empty((T, H), dtype=torch.float32, device=dev) if want_hidden else None
+        x = torch.empty((T, H), dtype=torch.bfloat16, device=dev) if want_x else None
+        x_q = torch.empty((T, H), dtype=torch.int8, device=dev)
+        x_scale = torch.empty(T, dtype=torch.float32, device=dev)
+    _check(_lib().moe_add_rmsnorm_i8(T, H, ph, pd, pg, float(eps), None if hs is None else hs.data_ptr(), None if x is None else x.data_ptr(), x_q.data_ptr(),
+                                     x_scale.data_ptr(), _stream(stream)), "moe_add_rmsnorm_i8")
+    return hs, x, x_q, x_scale
+
+
+def moe_linear_i8(ls: LinearShape, x_q, x_scale, page_table, page_pool, w_scale, status=None, stream=None) -> torch.Tensor:
+    """x_q int8 [T, K], x_scale float32 [T], w_scale float32 [N] -> float32 [T, N]"""
+    px = _dev(x_q, torch.int8, (ls.T, ls.K), "x_q")
+    pxs = _dev(x_scale, torch.float32, (ls.T,), "x_scale")
+    pt = _dev(page_table, torch.int32, (linear_pages_required(ls),), "page_table")
+    pp = _pool(page_pool, ls.page_bytes)
+    pw = _dev(w_scale, torch.float32, (ls.N,), "w_scale")
+    ps = _optional(status, torch.int32, (4,), "status")
+    with _on(stream):
+        out = torch.empty((ls.T, ls.N), dtype=torch.float32, device=x_q.device)
+    _check(_lib().moe_linear_i8(ctypes.byref(ls), px, pxs, pt, pp, int(page_pool.shape[0]), pw, out.data_ptr(), ps, _stream(stream)), "moe_linear_i8")
+    return out
+
+
+def moe_expert_ffn_i8(s: MoEShape, x_q, x_scale, offsets, page_table, page_pool, scales: ExpertScales, row_src=None, row_w=None, status=None, stream=None):
+    """x_q int8 [T, H] with row_src, else [R, H] -> (h_q int8 [R, F], h_scale float32 [R], out bf16 [R, H])"""
+    R = s.R
+    rows = R if row_src is None else s.T
+    gu, d = pages_required(s)
+    px = _dev(x_q, torch.int8, (rows, s.H), "x_q")
+    pxs = _dev(x_scale, torch.float32, (rows,), "x_scale")
+    pr = _optional(row_src, torch.int32, (R,), "row_src")
+    po = _dev(offsets, torch.int32, (s.E + 1,), "offsets")
+    pt = _dev(page_table, torch.int32, (s.E, gu + d), "page_table")
+    pp = _pool(page_pool, s.page_bytes)
+    pw = _optional(row_w, torch.float32, (R,), "row_w")
+    ps = _optional(status, torch.int32, (4,), "status")
+    with _on(stream):
+        h = torch.empty((R, s.F), dtype=torch.bfloat16, device=x_q.device)
+        h_q = torch.empty((R, s.F), dtype=torch.int8, device=x_q.device)
+        h_scale = torch.empty(R, dtype=torch.float32, device=x_q.device)
+        out = torch.empty((R, s.H), dtype=torch.bfloat16, device=x_q.device)
+    _check(_lib().moe_expert_ffn_i8(ctypes.byref(s), px, pxs, pr, po, pt, pp, int(page_pool.shape[0]), scales.pointers(s), pw, h.data_ptr(), h_q.data_ptr(),
+                                    h_scale.data_ptr(), out.data_ptr(), ps, _stream(stream)), "moe_expert_ffn_i8")
+    return h_q, h_scale, out
+
+
+@functools.lru_cache(maxsize=256)
+def _layer_i8_workspace_bytes(*fields):
+    v = _sz(0)
+    _check(_lib().moe_layer_i8_workspace_bytes(ctypes.byref(MoEShape(*fields)), ctypes.byref(v)), "moe_layer_i8_workspace_bytes")
+    return int(v.value)
+
+
+def layer_i8_workspace_bytes(s: MoEShape) -> int:
+    return _layer_i8_workspace_bytes(s.T, s.H, s.F, s.E, s.k, s.dtype, s.page_bytes)
+
+
+def _scratch(nbytes: int, device) -> torch.Tensor:
+    ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    if ws.data_ptr() % 256:
+        raise RuntimeError("allocator returned an unaligned workspace")
+    return ws
+
+
+def moe_layer_i8(s: MoEShape, x, x_q, x_scale, Wr, page_table, page_pool, scales: ExpertScales, bias=None, workspace: Optional[torch.Tensor] = None,
+                 y: Optional[torch.Tensor] = None, stream=None):
+    """x bf16 [T, H] for the router, the same rows in 8 bits for the experts (both of moe_add_rmsnorm_i8)
+    -> (y float32 [T, H], workspace uint8, its first int32 the status word)"""
+    gu, d = pages_required(s)
+    px = _dev(x, torch.bfloat16, (s.T, s.H), "x")
+    pq = _dev(x_q, torch.int8, (s.T, s.H), "x_q")
+    pqs = _dev(x_scale, torch.float32, (s.T,), "x_scale")
+    pw = _dev(Wr, torch.bfloat16, (s.E, s.H), "Wr")
+    pb = _optional(bias, torch.float32, (s.E,), "bias")
+    pt = _dev(page_table, torch.int32, (s.E, gu + d), "page_table")
+    pp = _pool(page_pool, s.page_bytes)
+    if workspace is None or y is None:
+        with _on(stream):
+            workspace = _scratch(layer_i8_workspace_bytes(s), x.device) if workspace is None else workspace
+            y = torch.empty((s.T, s.H), dtype=torch.float32, device=x.device) if y is None else y
+    py = _dev(y, torch.float32, (s.T, s.H), "y")
+    pws = _dev(workspace, torch.uint8, None, "workspace")
+    _check(_lib().moe_layer_i8(ctypes.byref(s), px, pq, pqs, pw, pb, pt, pp, int(page_pool.shape[0]), scales.pointers(s), py, pws, workspace.numel(), _stream(stream)),
+           "moe_layer_i8")
+    return y, workspace
+
+
+def moe_pre_attention_i8(qkv_proj: LinearShape, hidden, delta, norm_gamma, eps, qkv_table, page_pool, qkv_scale, status=None, stream=None):
+    """-> (hidden_out float32 [T, K], x_q int8 [T, K], x_scale float32 [T], qkv float32 [T, N])"""
+    shape = (qkv_proj.T, qkv_proj.K)
+    ph = _optional(hidden, torch.float32, shape, "hidden")
+    pd = _dev(delta, torch.float32, shape, "delta")
+    pg = _dev(norm_gamma, torch.float32, shape[1:], "norm_gamma")
+    pt = _dev(qkv_table, torch.int32, (linear_pages_required(qkv_proj),), "qkv_table")
+    pp = _pool(page_pool, qkv_proj.page_bytes)
+    pw = _dev(qkv_scale, torch.float32, (qkv_proj.N,), "qkv_scale")
+    ps = _optional(status, torch.int32, (4,), "status")
+    dev = delta.device
+    with _on(stream):
+        hidden_out = torch.empty(shape, dtype=torch.float32, device=dev)
+        x_q = torch.empty(shape, dtype=torch.int8, device=dev)
+        x_scale = torch.empty(shape[0], dtype=torch.float32, device=dev)
+        qkv = torch.empty((qkv_proj.T, qkv_proj.N), dtype=torch.float32, device=dev)
+    _check(_lib().moe_pre_attention_i8(ctypes.byref(qkv_proj), ph, pd, pg, float(eps), pt, pp, int(page_pool.shape[0]), pw, hidden_out.data_ptr(), x_q.data_ptr(),
+                                       x_scale.data_ptr(), qkv.data_ptr(), ps, _stream(stream)), "moe_pre_attention_i8")
+    return hidden_out, x_q, x_scale, qkv
+
+
+def post_attention_i8_workspace_bytes(s: MoEShape, o_proj: LinearShape) -> int:
+    v = _sz(0)
+    _check(_lib().moe_post_attention_i8_workspace_bytes(ctypes.byref(s), ctypes.byref(o_proj), ctypes.byref(v)), "moe_post_attention_i8_workspace_bytes")
+    return int(v.value)
+
+
+def moe_post_attention_i8(s: MoEShape, o_proj: LinearShape, attn, hidden, o_table, o_scale, norm_gamma, eps, Wr, page_table, page_pool, scales: ExpertScales, bias=None,
+                          workspace: Optional[torch.Tensor] = None, stream=None):
+    """-> (hidden_mid float32, x_moe bf16, y float32, all [T, H], workspace uint8, its first int32 the status word)"""
+    gu, d = pages_required(s)
+    pa = _dev(attn, torch.bfloat16, (s.T, o_proj.K), "attn")
+    ph = _dev(hidden, torch.float32, (s.T, s.H), "hidden")
+    po = _dev(o_table, torch.int32, (linear_pages_required(o_proj),), "o_table")
+    pos = _dev(o_scale, torch.float32, (o_proj.N,), "o_scale")
+    pg = _dev(norm_gamma, torch.float32, (s.H,), "norm_gamma")
+    pw = _dev(Wr, torch.bfloat16, (s.E, s.H), "Wr")
+    pb = _optional(bias, torch.float32, (s.E,), "bias")
+    pt = _dev(page_table, torch.int32, (s.E, gu + d), "page_table")
+    pp = _pool(page_pool, s.page_bytes)
+    dev = attn.device
+    with _on(stream):
+        hidden_mid = torch.empty((s.T, s.H), dtype=torch.float32, device=dev)
+        x_moe = torch.empty((s.T, s.H), dtype=torch.bfloat16, device=dev)
+        y = torch.empty((s.T, s.H), dtype=torch.float32, device=dev)
+        workspace = _scratch(post_attention_i8_workspace_bytes(s, o_proj), dev) if workspace is None else workspace
+    pws = _dev(workspace, torch.uint8, None, "workspace")
+    _check(_lib().moe_post_attention_i8(ctypes.byref(s), ctypes.byref(o_proj), pa, ph, po, pos, pg, float(eps), pw, pb, pt, pp, int(page_pool.shape[0]),
+                                        scales.pointers(s), hidden_mid.data_ptr(), x_moe.data_ptr(), y.data_ptr(), pws, workspace.numel(), _stream(stream)),
+           "moe_post_attention_i8")
+    return hidden_mid, x_moe, y, workspace
 
 
 # ----------------------------------------------------------------------------- attention over a paged key-value cache

@@ -45,7 +45,7 @@ def check_kernel_assembly(asm_path: str) -> None:
     with open(asm_path) as f:
         for line in f:
             code = line.split(";")[0]
-            if re.match(r"^_Z\w*ffn_gemm_bf16\w*:", code):
+            if re.match(r"^_Z\w*ffn_gemm\w*:", code):
                 in_kernel = True
             elif code.startswith(".Lfunc_end"):
                 in_kernel = False

@@ -126,7 +126,7 @@ static int layer_body(const moe_shape& s, const void* x, const void* Wr, const f
     if (rc != MOE_OK) return rc;
     prof_mark(ps, 4, st);
     // the gate weight was applied in the down-projection epilogue: plain sum here
-    rc = launch_combine(s, (const float*)(ws + L.out), row_of, nullptr, y, st);
+    rc = launch_combine(s, ws + L.out, row_of, nullptr, y, st);
     prof_mark(ps, 5, st);
     return rc;
 }
@@ -157,7 +157,7 @@ extern "C" {
 int moe_last_hip_error(void) { return g_last_hip_error; }
 
 int moe_workspace_layout_get(const moe_shape* s, moe_workspace_layout* out) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (!out) return MOE_ERR_INVALID_ARG;
     return layout(*s, out);
@@ -165,7 +165,7 @@ int moe_workspace_layout_get(const moe_shape* s, moe_workspace_layout* out) {
 
 int moe_route(const moe_shape* s, const void* x, const void* Wr, const float* bias,
               int32_t* topk_ids, float* topk_w, float* logits, void* stream) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (s->T == 0) return MOE_OK;
     if (!x || !Wr || !topk_ids || !topk_w) return MOE_ERR_INVALID_ARG;
@@ -175,7 +175,7 @@ int moe_route(const moe_shape* s, const void* x, const void* Wr, const float* bi
 int moe_permute(const moe_shape* s, const int32_t* topk_ids, const float* topk_w, const void* x,
                 int32_t* counts, int32_t* offsets, int32_t* row_src, int32_t* row_of,
                 float* row_w, void* x_perm, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (!counts || !offsets) return MOE_ERR_INVALID_ARG;
     if (s->T > 0 && (!topk_ids || !row_src || !row_of)) return MOE_ERR_INVALID_ARG;
@@ -190,7 +190,7 @@ int moe_permute(const moe_shape* s, const int32_t* topk_ids, const float* topk_w
 int moe_expert_ffn(const moe_shape* s, const void* x_perm, const int32_t* offsets,
                    const int32_t* page_table, const void* page_pool, int64_t pool_pages,
                    const float* row_w, void* h_ws, float* out, int32_t* status, void* stream) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (s->T == 0) return MOE_OK;
     if (!x_perm || !offsets || !page_table || !page_pool || !h_ws || !out || pool_pages <= 0)
@@ -200,7 +200,7 @@ int moe_expert_ffn(const moe_shape* s, const void* x_perm, const int32_t* offset
     return launch_expert_ffn(*s, a, (hipStream_t)stream);
 }
 
-int moe_combine(const moe_shape* s, const float* out, const int32_t* row_of,
+int moe_combine(const moe_shape* s, const void* out, const int32_t* row_of,
                 const float* topk_w, float* y, void* stream) {
     int rc = validate_shape(s);
     if (rc != MOE_OK) return rc;
@@ -212,7 +212,7 @@ int moe_combine(const moe_shape* s, const float* out, const int32_t* row_of,
 int moe_layer(const moe_shape* s, const void* x, const void* Wr, const float* bias,
               const int32_t* page_table, const void* page_pool, int64_t pool_pages,
               float* y, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (s->T == 0) return MOE_OK;
     if (!x || !Wr || !page_table || !page_pool || !y || !workspace || pool_pages <= 0)
@@ -253,7 +253,7 @@ extern "C" {
 int moe_layer_static(const moe_shape* s, const void* x, const void* Wr, const float* bias,
                      const int32_t* page_table, const void* page_pool, int64_t pool_pages,
                      float* y, void* stream) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (s->T == 0) return MOE_OK;
     if (!x || !Wr || !page_table || !page_pool || !y || pool_pages <= 0) return MOE_ERR_INVALID_ARG;
@@ -331,7 +331,7 @@ extern "C" {
 int moe_stream_create(const moe_shape* s, const void* host_pages, int64_t host_pool_pages,
                       const int32_t* host_page_table, void* slots, int32_t* slot_table,
                       moe_streamer** out) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (!host_pages || !host_page_table || !slots || !slot_table || !out || host_pool_pages <= 0)
         return MOE_ERR_INVALID_ARG;

@@ -1,13 +1,19 @@
 // a4. Un-permute and combine: y[t] = sum_slot w[t][slot] * out[row_of[t*k+slot]].
-// Pure HBM traffic (read R*H floats, write T*H floats): one block per token,
-// 16-byte loads along the row, the k rows of a token summed in slot order so the
+// Pure HBM traffic (read R*H floats, or bf16 behind 8-bit products, write T*H floats): one block per token,
+// four elements at a time along the row, the k rows of a token summed in slot order so the
 // result does not depend on scheduling.
 #include "moe_internal.h"
 
 namespace moe {
 namespace {
 
-__global__ __launch_bounds__(256) void combine_kernel(const float4* __restrict__ out, const int32_t* __restrict__ row_of,
+__device__ __forceinline__ float4 as_floats(const float4& v) { return v; }
+__device__ __forceinline__ float4 as_floats(const uint2& v) {        // four bf16
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+}
+
+template <class Four>
+__global__ __launch_bounds__(256) void combine_kernel(const Four* __restrict__ out, const int32_t* __restrict__ row_of,
                                                       const float* __restrict__ topk_w, int k, int R, int row_vec,
                                                       float4* __restrict__ y) {
     const int t = blockIdx.x;
@@ -22,7 +28,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const float4* __restrict__
     for (int c = threadIdx.x; c < row_vec; c += 256) {
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int s = 0; s < k; ++s) {
-            const float4 v = out[(size_t)rows[s] * row_vec + c];
+            const float4 v = as_floats(out[(size_t)rows[s] * row_vec + c]);
             const float ws = wts[s];
             acc.x = fmaf(ws, v.x, acc.x);
             acc.y = fmaf(ws, v.y, acc.y);
@@ -35,10 +41,12 @@ __global__ __launch_bounds__(256) void combine_kernel(const float4* __restrict__
 
 }  // namespace
 
-int launch_combine(const moe_shape& s, const float* out, const int32_t* row_of, const float* topk_w, float* y,
+int launch_combine(const moe_shape& s, const void* out, const int32_t* row_of, const float* topk_w, float* y,
                    hipStream_t st) {
-    hipLaunchKernelGGL(combine_kernel, dim3(s.T), dim3(256), 0, st, (const float4*)out, row_of, topk_w, s.k,
-                       s.T * s.k, s.H / 4, (float4*)y);
+    if (s.dtype == MOE_DTYPE_I8)
+        hipLaunchKernelGGL(combine_kernel<uint2>, dim3(s.T), dim3(256), 0, st, (const uint2*)out, row_of, topk_w, s.k, s.T * s.k, s.H / 4, (float4*)y);
+    else
+        hipLaunchKernelGGL(combine_kernel<float4>, dim3(s.T), dim3(256), 0, st, (const float4*)out, row_of, topk_w, s.k, s.T * s.k, s.H / 4, (float4*)y);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }

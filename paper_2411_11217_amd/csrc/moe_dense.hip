@@ -101,7 +101,7 @@ extern "C" {
 
 int moe_linear(const moe_linear_shape* s, const void* x, const int32_t* page_table, const void* page_pool,
                int64_t pool_pages, float* out, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
-    int rc = validate_linear(s);
+    int rc = validate_bf16_linear(s);
     if (rc != MOE_OK) return rc;
     if (s->T == 0) return MOE_OK;
     if (!x || !page_table || !page_pool || !out || !workspace || pool_pages <= 0) return MOE_ERR_INVALID_ARG;
@@ -128,9 +128,9 @@ int moe_post_attention(const moe_shape* s, const moe_linear_shape* o_proj, const
                        const int32_t* o_table, const float* norm_gamma, float eps, const void* Wr, const float* bias,
                        const int32_t* page_table, const void* page_pool, int64_t pool_pages,
                        float* hidden_mid, void* x_moe, float* y, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
-    rc = validate_linear(o_proj);
+    rc = validate_bf16_linear(o_proj);
     if (rc != MOE_OK) return rc;
     if (s->dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED_DTYPE;
     if (o_proj->T != s->T || o_proj->N != s->H || o_proj->page_bytes != s->page_bytes || s->H > 4 * kNormThreads * kMaxVec)
@@ -158,7 +158,7 @@ int moe_pre_attention(const moe_linear_shape* qkv_proj, const float* hidden, con
                       float eps, const int32_t* qkv_table, const void* page_pool, int64_t pool_pages,
                       float* hidden_out, void* x_norm, float* qkv, void* qkv_bf16, void* workspace, size_t workspace_bytes,
                       void* stream) {
-    int rc = validate_linear(qkv_proj);
+    int rc = validate_bf16_linear(qkv_proj);
     if (rc != MOE_OK) return rc;
     if (qkv_proj->K > 4 * kNormThreads * kMaxVec) return MOE_ERR_INVALID_ARG;
     if (qkv_proj->T == 0) return MOE_OK;
@@ -179,7 +179,7 @@ int moe_pre_attention(const moe_linear_shape* qkv_proj, const float* hidden, con
 }
 
 int moe_post_attention_workspace_bytes(const moe_shape* s, size_t* bytes) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     if (!bytes) return MOE_ERR_INVALID_ARG;
     *bytes = (layer_workspace_bytes(*s) + 255) / 256 * 256 + 256 + (size_t)s->T * s->H * 4;

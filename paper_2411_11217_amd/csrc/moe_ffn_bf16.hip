@@ -1,5 +1,5 @@
 // a3, bf16 operands: which kernel a launch of the expert FFN or of the dense linear map takes.
-#include "moe_ffn_gemm_bf16.h"
+#include "moe_ffn_gemm.h"
 
 namespace moe {
 
@@ -29,7 +29,7 @@ int launch_expert_ffn_bf16(const moe_shape& s, const Geom& g, const FfnArgs& a, 
         const int64_t last = n_exp * row_tiles_each * p.NT % kComputeUnits;
         return last != 0 && last <= kComputeUnits / 2;
     };
-    const int rc = half_round() ? launch_gate_up_halves_bf16(p, R, n_exp, st) : launch_stages<0, 2>(p, R, n_exp, st);
+    const int rc = half_round() ? launch_gate_up_halves_bf16(p, R, n_exp, st) : launch_stages<Bf16, 0, 2>(p, R, n_exp, st);
     if (rc != MOE_OK) return rc;
     if (a.mid_event) MOE_HIP_TRY(hipEventRecord(a.mid_event, st));
     fill_down(p, s, g, a);
@@ -48,9 +48,9 @@ int launch_expert_ffn_bf16(const moe_shape& s, const Geom& g, const FfnArgs& a, 
     if (opt == 1 || (opt == 0 && narrow_tiles <= kComputeUnits)) {
         p.NT = (int32_t)g.dt;
         if (narrow_tiles <= kComputeUnits / 2) return launch_down_narrow_halves_bf16(p, R, n_exp, st);
-        return launch_stages<1, 1>(p, R, n_exp, st);
+        return launch_stages<Bf16, 1, 1>(p, R, n_exp, st);
     }
-    return half_round() ? launch_down_halves_bf16(p, R, n_exp, st) : launch_stages<1, 2>(p, R, n_exp, st);
+    return half_round() ? launch_down_halves_bf16(p, R, n_exp, st) : launch_stages<Bf16, 1, 2>(p, R, n_exp, st);
 }
 
 // y = x W^T for a dense weight matrix held as pages: one of the two down-projection kernels (linear_takes_rows_kernel in
@@ -103,13 +103,13 @@ int launch_linear_bf16(const LinearArgs& a, hipStream_t st) {
         const int64_t half_tiles = (int64_t)((a.T + 127) / 128) * p.NT;
         if (p.half_tiles && a.T > 128 && half_tiles <= kComputeUnits && (a.T > 160 || half_tiles <= 224 || p.KT <= 32)) {
             p.tall_rows = 0;
-            rc = launch_stages<1, 1, 128>(p, a.T, 1, st);
+            rc = launch_stages<Bf16, 1, 1, 128>(p, a.T, 1, st);
         } else {
-            rc = launch_stages<1, 1>(p, a.T, 1, st);
+            rc = launch_stages<Bf16, 1, 1>(p, a.T, 1, st);
         }
     } else {
         p.NT = wide_tiles;
-        rc = launch_stages<1, 2>(p, a.T, 1, st);
+        rc = launch_stages<Bf16, 1, 2>(p, a.T, 1, st);
     }
     if (rc != MOE_OK || !a.out16) return rc;
     return launch_cast_bf16((int64_t)a.T * a.N, a.out, a.out16, st);

@@ -1,4 +1,4 @@
-// Pieces shared by the expert-FFN GEMM kernels (bf16 and f32): the launch
+// Pieces shared by the expert-FFN GEMM kernels (bf16, f32 and 8-bit integers): the launch
 // parameter block, the block -> (expert, row tile, column tile) map and the
 // page-table lookup of a weight tile.
 #pragma once
@@ -42,6 +42,10 @@ struct GemmParams {
     int32_t tall_first;       // bf16 kernel: tile numbering with the tall tiles of a chunk of groups first, see locate_tile
     int32_t stream;           // bf16 kernels: experts with one row tile load their weights and store h with the non-temporal hint; 2: all experts h
     int32_t balance;          // 1: no XCD runs more than an eighth of the launch's tiles, see stolen_tile
+    // 8-bit integers:
+    const float* a_scale;     // of each row of the matrix at A
+    const float* w_scale;     // of each output column, [E][n_cols] (MODE 0: of the gate matrix's)
+    const float* w_scale_up;  // MODE 0: of the up matrix's
 };
 
 constexpr int kXcdUnits = 32;                        // compute units of an XCD
@@ -260,12 +264,12 @@ __device__ __forceinline__ float silu_mul_bf16(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
 }
 
-// the kernel for few rows per expert (moe_ffn_rows_bf16.hip); p as filled for the launch, NT is set there
+// the kernel for few rows per expert (moe_ffn_rows.h); p as filled for the launch, NT is set there
 bool rows_kernel_takes(int rows_each);
 int launch_gate_up_rows_bf16(GemmParams& p, int F, int R, int rows_each, int n_exp, hipStream_t st);
 int launch_down_rows_bf16(GemmParams& p, int H, int R, int rows_each, int n_exp, hipStream_t st);
 int launch_linear_rows_bf16(GemmParams& p, int N, int T, hipStream_t st);
-// the one for a handful of tokens (moe_ffn_thin_bf16.hip)
+// the one for a handful of tokens (moe_ffn_thin.h)
 bool thin_takes_gate_up(const moe_shape& s);
 bool thin_takes_down(const moe_shape& s);
 int launch_gate_up_thin_bf16(GemmParams& p, int F, int R, int n_exp, hipStream_t st);

@@ -1,9 +1,11 @@
-// a3. Grouped SwiGLU expert FFN, bf16 operands, fp32 accumulation, on the CDNA4
-// matrix cores (v_mfma_f32_16x16x32_bf16), weights read through the page table.
+// a3. Grouped SwiGLU expert FFN on the CDNA4 matrix cores, weights read through the page table: bf16 operands with
+// fp32 sums (v_mfma_f32_16x16x32_bf16), or 8-bit integers with scales (v_mfma_i32_16x16x64_i8; moe_ffn_op.h).  Where
+// this file counts elements along k they are bf16; of integers there are twice as many in the same bytes.
 //
 // Two launches of one kernel template:
 //   MODE 0 (gate/up):  [g | u] = x_perm . [W1_e ; W3_e]^T,  h = bf16(silu(g) * u)
 //   MODE 1 (down):     out     = h . W2_e^T  (* row weight)
+// With integers the sums are multiplied by the scales of their row and column first, and out is bf16 or float32.
 //
 // Work decomposition.  A block owns a 256-row x 256-column piece of one expert's
 // output.  Its columns are two page tiles (128 output features each): for MODE 0
@@ -67,14 +69,13 @@
 #include <utility>
 
 #include "moe_ffn_common.h"
+#include "moe_ffn_op.h"
 
 namespace moe {
 namespace {
 
 #define MOE_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));        // an MFMA operand: 8 bf16 in four registers
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(1))) const void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
@@ -82,7 +83,7 @@ constexpr int BM = 256;
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kComputeUnits = 256;           // MI355X
-// Up to this many rows per expert on average the weight loads are non-temporal, here and in moe_ffn_rows_bf16.hip: an expert
+// Up to this many rows per expert on average the weight loads are non-temporal, here and in moe_ffn_rows.h: an expert
 // is one row tile then, every weight is read once, and a line that will not be read again should not push others out.  A
 // kernel of nothing but loads reads 7.1 TB/s with the hint and 6.2 without (moe_probe_stream_read_nt).  Layer without / with,
 // us: Mixtral-8x7B shape 16 tokens 481 / 434, 64: 487 / 444, 256: 520 / 491 (these in the other kernel), 400: 544 / 529, 700:
@@ -93,7 +94,7 @@ constexpr int kComputeUnits = 256;           // MI355X
 // And only where the experts' weights exceed the 256 MiB last-level cache: smaller ones may still be there from the call
 // before, and the hint keeps them out (8 experts of 1024 x 2816, 138 MB, 100 tokens: 53 without, 56 with).  Where other
 // weights pass in between it is the other way round (ten such layers in turn, 8 tokens 49 / 47, 100: 55 / 53, 400: 70 / 69).
-// The same experts store h with the hint (here and in moe_ffn_rows_bf16.hip): lines written through as they come cost the reads of the
+// The same experts store h with the hint (here and in moe_ffn_rows.h): lines written through as they come cost the reads of the
 // weights less than dirty lines that the end of the launch has to write back.  (Any write does: a kernel of nothing but loads that
 // reads 1.88 GB in 274 us takes 300 when its blocks also write 15 MB, wherever these go.)  Gate/up launch without / with, us: Mixtral-8x7B
 // shape 256 tokens 323 / 304, 1000: 443 / 435 (and the down launch behind it 257 / 251); DBRX shape, 600 tokens 784 / 762; layer of
@@ -125,7 +126,7 @@ __device__ __forceinline__ void wait_loads_and_lds() {
 
 // D = A * B + D on a 16 x 16 tile over 32 k (v_mfma_f32_16x16x32_bf16): lane l holds row l % 16 of A
 // and column l % 16 of B, each the 8 elements k = (l / 16) * 8 .. + 7, and D[(l / 16) * 4 + r][l % 16] in
-// register r of the tile's four.
+// register r of the tile's four.  (v_mfma_i32_16x16x64_i8: 16 elements k = (l / 16) * 16 .. + 15, the same D as whole numbers.)
 //
 // The accumulators are the accumulator registers a0 .. a255 (a0 .. a127 for the narrow block) NAMED in
 // inline assembly, tile t in a[4t : 4t + 3]; the compiler never sees them as values.  With the
@@ -141,10 +142,13 @@ __device__ __forceinline__ void acc_declare() {
     else asm volatile("" ::: "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", "a10", "a11", "a12", "a13", "a14", "a15", "a16", "a17", "a18", "a19", "a20", "a21", "a22", "a23", "a24", "a25", "a26", "a27", "a28", "a29", "a30", "a31", "a32", "a33", "a34", "a35", "a36", "a37", "a38", "a39", "a40", "a41", "a42", "a43", "a44", "a45", "a46", "a47", "a48", "a49", "a50", "a51", "a52", "a53", "a54", "a55", "a56", "a57", "a58", "a59", "a60", "a61", "a62", "a63", "a64", "a65", "a66", "a67", "a68", "a69", "a70", "a71", "a72", "a73", "a74", "a75", "a76", "a77", "a78", "a79", "a80", "a81", "a82", "a83", "a84", "a85", "a86", "a87", "a88", "a89", "a90", "a91", "a92", "a93", "a94", "a95", "a96", "a97", "a98", "a99", "a100", "a101", "a102", "a103", "a104", "a105", "a106", "a107", "a108", "a109", "a110", "a111", "a112", "a113", "a114", "a115", "a116", "a117", "a118", "a119", "a120", "a121", "a122", "a123", "a124", "a125", "a126", "a127");
 #endif
 }
-template <int R>
-__device__ __forceinline__ void mfma_16x16x32(const i32x4& a, const i32x4& b) {     // tile in a[R : R + 3]
+#define MOE_MFMA_BF16 "v_mfma_f32_16x16x32_bf16"
+#define MOE_MFMA_I8 "v_mfma_i32_16x16x64_i8"
+template <class Op, int R>
+__device__ __forceinline__ void mfma_16x16(const i32x4& a, const i32x4& b) {     // tile in a[R : R + 3]
 #ifdef __HIP_DEVICE_COMPILE__
-    asm volatile("v_mfma_f32_16x16x32_bf16 a[%2:%3], %0, %1, a[%2:%3]" ::"v"(a), "v"(b), "n"(R), "n"(R + 3));
+    if constexpr (Op::kScaled) asm volatile(MOE_MFMA_I8 " a[%2:%3], %0, %1, a[%2:%3]" ::"v"(a), "v"(b), "n"(R), "n"(R + 3));
+    else asm volatile(MOE_MFMA_BF16 " a[%2:%3], %0, %1, a[%2:%3]" ::"v"(a), "v"(b), "n"(R), "n"(R + 3));
 #endif
 }
 // The same MFMA with one global -> LDS load of 16 bytes per lane behind it: LDS address
@@ -155,37 +159,28 @@ __device__ __forceinline__ void mfma_16x16x32(const i32x4& a, const i32x4& b) { 
 // (The compiler puts an s_nop in front of every such statement that follows another within a few instructions, because
 // M0 is on the clobber list: six per half-step.  They issue in the shadow of an MFMA: a build without the clobber,
 // and so without them, was not faster.)
-template <int R, int LDS_IMM, bool STREAM>
-__device__ __forceinline__ void mfma_16x16x32_then_load(const i32x4& a, const i32x4& b, const char* base, uint32_t offset, uint32_t lds_base) {
+#define MOE_MFMA_THEN_LOAD(MFMA, HINT)                                                                                              \
+    asm volatile("s_add_i32 m0, %4, %5\n\t" MFMA " a[%6:%7], %0, %1, a[%6:%7]\n\tglobal_load_lds_dwordx4 %2, %3" HINT                \
+                 ::"v"(a), "v"(b), "v"(offset), "s"(base), "s"(lds_base), "n"(LDS_IMM), "n"(R), "n"(R + 3)                          \
+                 : "memory", "m0")
+template <class Op, int R, int LDS_IMM, bool STREAM>
+__device__ __forceinline__ void mfma_16x16_then_load(const i32x4& a, const i32x4& b, const char* base, uint32_t offset, uint32_t lds_base) {
 #ifdef __HIP_DEVICE_COMPILE__
-    if constexpr (STREAM)
-        asm volatile("s_add_i32 m0, %4, %5\n\tv_mfma_f32_16x16x32_bf16 a[%6:%7], %0, %1, a[%6:%7]\n\tglobal_load_lds_dwordx4 %2, %3 nt"
-                     ::"v"(a), "v"(b), "v"(offset), "s"(base), "s"(lds_base), "n"(LDS_IMM), "n"(R), "n"(R + 3)
-                     : "memory", "m0");
-    else
-        asm volatile("s_add_i32 m0, %4, %5\n\tv_mfma_f32_16x16x32_bf16 a[%6:%7], %0, %1, a[%6:%7]\n\tglobal_load_lds_dwordx4 %2, %3"
-                     ::"v"(a), "v"(b), "v"(offset), "s"(base), "s"(lds_base), "n"(LDS_IMM), "n"(R), "n"(R + 3)
-                     : "memory", "m0");
+    if constexpr (Op::kScaled && STREAM) MOE_MFMA_THEN_LOAD(MOE_MFMA_I8, " nt");
+    else if constexpr (Op::kScaled) MOE_MFMA_THEN_LOAD(MOE_MFMA_I8, "");
+    else if constexpr (STREAM) MOE_MFMA_THEN_LOAD(MOE_MFMA_BF16, " nt");
+    else MOE_MFMA_THEN_LOAD(MOE_MFMA_BF16, "");
 #endif
 }
-// The same MFMA with its accumulator tile in vector registers the compiler allocates, and a plain 16-byte load
-// into vector registers: the tall tiles' extra row tile.  The load is not known to the compiler's wait counting;
-// its result is used only behind a wait that covers it.
-__device__ __forceinline__ void mfma_16x16x32_v(f32x4& acc, const i32x4& a, const i32x4& b) {
-#ifdef __HIP_DEVICE_COMPILE__
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b));
-#endif
-}
+// The tall tiles' extra row tile has its accumulators in vector registers the compiler allocates, and its row fragment comes by a plain 16-byte load
+// into vector registers.  The load is not known to the compiler's wait counting; its result is used only behind a wait that covers it.
 // The MFMAs of a tall tile's extra row tile, all in ONE statement: acc[j] += a * b[j] for the column fragments that
 // `which` selects - 0: all of them; 1 / 2: the first / second half of a split (see the kernel), i.e. with GATE_UP the
 // gate fragments 0, 1 (2, 3) and their up fragments 4, 5 (6, 7), else fragments 0 .. NJ/2-1 (NJ/2 .. NJ-1).  The choice
 // is a branch INSIDE the statement: the compiler sees one unconditional read-modify-write of all accumulator tiles and
 // has no control flow to merge them across (with a branch in the source it copied the tiles next to the MFMAs that
 // were still writing them).
-template <bool GATE_UP>
-__device__ __forceinline__ void mfma_extra_tile_8(f32x4 (&acc)[8], const i32x4& a, const i32x4 (&b)[8], int which) {
-#ifdef __HIP_DEVICE_COMPILE__
-#define MOE_XM(J) "v_mfma_f32_16x16x32_bf16 %" #J ", %8, %" MOE_XB_##J ", %" #J "\n\t"
+#define MOE_XM(MFMA, J) MFMA " %" #J ", %8, %" MOE_XB_##J ", %" #J "\n\t"
 #define MOE_XB_0 "9"
 #define MOE_XB_1 "10"
 #define MOE_XB_2 "11"
@@ -194,75 +189,66 @@ __device__ __forceinline__ void mfma_extra_tile_8(f32x4 (&acc)[8], const i32x4& 
 #define MOE_XB_5 "14"
 #define MOE_XB_6 "15"
 #define MOE_XB_7 "16"
-    if constexpr (GATE_UP) {
-        asm volatile("s_cmp_lg_u32 %17, 0\n\ts_cbranch_scc1 1f\n\t"
-                     MOE_XM(0) MOE_XM(1) MOE_XM(2) MOE_XM(3) MOE_XM(4) MOE_XM(5) MOE_XM(6) MOE_XM(7)
-                     "s_branch 3f\n1:\n\ts_cmp_lg_u32 %17, 1\n\ts_cbranch_scc1 2f\n\t"
-                     MOE_XM(0) MOE_XM(1) MOE_XM(4) MOE_XM(5)
-                     "s_branch 3f\n2:\n\t"
-                     MOE_XM(2) MOE_XM(3) MOE_XM(6) MOE_XM(7)
-                     "3:\n\t"
-                     : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]), "+v"(acc[4]), "+v"(acc[5]), "+v"(acc[6]), "+v"(acc[7])
-                     : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "s"(which)
-                     : "scc");
-    } else {
-        asm volatile("s_cmp_lg_u32 %17, 0\n\ts_cbranch_scc1 1f\n\t"
-                     MOE_XM(0) MOE_XM(1) MOE_XM(2) MOE_XM(3) MOE_XM(4) MOE_XM(5) MOE_XM(6) MOE_XM(7)
-                     "s_branch 3f\n1:\n\ts_cmp_lg_u32 %17, 1\n\ts_cbranch_scc1 2f\n\t"
-                     MOE_XM(0) MOE_XM(1) MOE_XM(2) MOE_XM(3)
-                     "s_branch 3f\n2:\n\t"
-                     MOE_XM(4) MOE_XM(5) MOE_XM(6) MOE_XM(7)
-                     "3:\n\t"
-                     : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]), "+v"(acc[4]), "+v"(acc[5]), "+v"(acc[6]), "+v"(acc[7])
-                     : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "s"(which)
-                     : "scc");
-    }
+#define MOE_EXTRA_8(MFMA, A0, A1, A2, A3, B0, B1, B2, B3)                                                                                              \
+    asm volatile("s_cmp_lg_u32 %17, 0\n\ts_cbranch_scc1 1f\n\t"                                                                                        \
+                 MOE_XM(MFMA, 0) MOE_XM(MFMA, 1) MOE_XM(MFMA, 2) MOE_XM(MFMA, 3) MOE_XM(MFMA, 4) MOE_XM(MFMA, 5) MOE_XM(MFMA, 6) MOE_XM(MFMA, 7)       \
+                 "s_branch 3f\n1:\n\ts_cmp_lg_u32 %17, 1\n\ts_cbranch_scc1 2f\n\t"                                                                     \
+                 MOE_XM(MFMA, A0) MOE_XM(MFMA, A1) MOE_XM(MFMA, A2) MOE_XM(MFMA, A3)                                                                   \
+                 "s_branch 3f\n2:\n\t"                                                                                                                 \
+                 MOE_XM(MFMA, B0) MOE_XM(MFMA, B1) MOE_XM(MFMA, B2) MOE_XM(MFMA, B3)                                                                   \
+                 "3:\n\t"                                                                                                                              \
+                 : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]), "+v"(acc[4]), "+v"(acc[5]), "+v"(acc[6]), "+v"(acc[7])                      \
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "s"(which)                          \
+                 : "scc")
+template <class Op, bool GATE_UP>
+__device__ __forceinline__ void mfma_extra_tile_8(typename Op::Acc (&acc)[8], const i32x4& a, const i32x4 (&b)[8], int which) {
+#ifdef __HIP_DEVICE_COMPILE__
+    if constexpr (Op::kScaled && GATE_UP) MOE_EXTRA_8(MOE_MFMA_I8, 0, 1, 4, 5, 2, 3, 6, 7);
+    else if constexpr (Op::kScaled) MOE_EXTRA_8(MOE_MFMA_I8, 0, 1, 2, 3, 4, 5, 6, 7);
+    else if constexpr (GATE_UP) MOE_EXTRA_8(MOE_MFMA_BF16, 0, 1, 4, 5, 2, 3, 6, 7);
+    else MOE_EXTRA_8(MOE_MFMA_BF16, 0, 1, 2, 3, 4, 5, 6, 7);
 #endif
 }
 // the same for the narrow block's four column fragments: halves 0, 1 and 2, 3, with GATE_UP 0, 2 and 1, 3
-template <bool GATE_UP>
-__device__ __forceinline__ void mfma_extra_tile_4(f32x4 (&acc)[4], const i32x4& a, const i32x4 (&b)[4], int which) {
+#define MOE_YM(MFMA, J, B) MFMA " %" #J ", %4, %" #B ", %" #J "\n\t"
+#define MOE_EXTRA_4(MFMA, FIRST, SECOND)                                                                                     \
+    asm volatile("s_cmp_lg_u32 %9, 0\n\ts_cbranch_scc1 1f\n\t"                                                               \
+                 MOE_YM(MFMA, 0, 5) MOE_YM(MFMA, 1, 6) MOE_YM(MFMA, 2, 7) MOE_YM(MFMA, 3, 8)                                 \
+                 "s_branch 3f\n1:\n\ts_cmp_lg_u32 %9, 1\n\ts_cbranch_scc1 2f\n\t"                                            \
+                 FIRST                                                                                                       \
+                 "s_branch 3f\n2:\n\t"                                                                                       \
+                 SECOND                                                                                                      \
+                 "3:\n\t"                                                                                                    \
+                 : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3])                                                    \
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "s"(which)                                            \
+                 : "scc")
+template <class Op, bool GATE_UP>
+__device__ __forceinline__ void mfma_extra_tile_4(typename Op::Acc (&acc)[4], const i32x4& a, const i32x4 (&b)[4], int which) {
 #ifdef __HIP_DEVICE_COMPILE__
-#define MOE_YM(J, B) "v_mfma_f32_16x16x32_bf16 %" #J ", %4, %" #B ", %" #J "\n\t"
-    if constexpr (GATE_UP) {
-        asm volatile("s_cmp_lg_u32 %9, 0\n\ts_cbranch_scc1 1f\n\t"
-                     MOE_YM(0, 5) MOE_YM(1, 6) MOE_YM(2, 7) MOE_YM(3, 8)
-                     "s_branch 3f\n1:\n\ts_cmp_lg_u32 %9, 1\n\ts_cbranch_scc1 2f\n\t"
-                     MOE_YM(0, 5) MOE_YM(2, 7)
-                     "s_branch 3f\n2:\n\t"
-                     MOE_YM(1, 6) MOE_YM(3, 8)
-                     "3:\n\t"
-                     : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3])
-                     : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "s"(which)
-                     : "scc");
-    } else {
-        asm volatile("s_cmp_lg_u32 %9, 0\n\ts_cbranch_scc1 1f\n\t"
-                     MOE_YM(0, 5) MOE_YM(1, 6) MOE_YM(2, 7) MOE_YM(3, 8)
-                     "s_branch 3f\n1:\n\ts_cmp_lg_u32 %9, 1\n\ts_cbranch_scc1 2f\n\t"
-                     MOE_YM(0, 5) MOE_YM(1, 6)
-                     "s_branch 3f\n2:\n\t"
-                     MOE_YM(2, 7) MOE_YM(3, 8)
-                     "3:\n\t"
-                     : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3])
-                     : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "s"(which)
-                     : "scc");
-    }
+    if constexpr (Op::kScaled && GATE_UP) MOE_EXTRA_4(MOE_MFMA_I8, MOE_YM(MOE_MFMA_I8, 0, 5) MOE_YM(MOE_MFMA_I8, 2, 7), MOE_YM(MOE_MFMA_I8, 1, 6) MOE_YM(MOE_MFMA_I8, 3, 8));
+    else if constexpr (Op::kScaled) MOE_EXTRA_4(MOE_MFMA_I8, MOE_YM(MOE_MFMA_I8, 0, 5) MOE_YM(MOE_MFMA_I8, 1, 6), MOE_YM(MOE_MFMA_I8, 2, 7) MOE_YM(MOE_MFMA_I8, 3, 8));
+    else if constexpr (GATE_UP) MOE_EXTRA_4(MOE_MFMA_BF16, MOE_YM(MOE_MFMA_BF16, 0, 5) MOE_YM(MOE_MFMA_BF16, 2, 7), MOE_YM(MOE_MFMA_BF16, 1, 6) MOE_YM(MOE_MFMA_BF16, 3, 8));
+    else MOE_EXTRA_4(MOE_MFMA_BF16, MOE_YM(MOE_MFMA_BF16, 0, 5) MOE_YM(MOE_MFMA_BF16, 1, 6), MOE_YM(MOE_MFMA_BF16, 2, 7) MOE_YM(MOE_MFMA_BF16, 3, 8));
 #endif
 }
 // and for the two column fragments of a block of 64 columns
-__device__ __forceinline__ void mfma_extra_tile_2(f32x4 (&acc)[2], const i32x4& a, const i32x4 (&b)[2], int which) {
+#define MOE_ZM(MFMA, J, B) MFMA " %" #J ", %2, %" #B ", %" #J "\n\t"
+#define MOE_EXTRA_2(MFMA)                                                                    \
+    asm volatile("s_cmp_lg_u32 %5, 0\n\ts_cbranch_scc1 1f\n\t"                               \
+                 MOE_ZM(MFMA, 0, 3) MOE_ZM(MFMA, 1, 4)                                       \
+                 "s_branch 3f\n1:\n\ts_cmp_lg_u32 %5, 1\n\ts_cbranch_scc1 2f\n\t"            \
+                 MOE_ZM(MFMA, 0, 3)                                                          \
+                 "s_branch 3f\n2:\n\t"                                                       \
+                 MOE_ZM(MFMA, 1, 4)                                                          \
+                 "3:\n\t"                                                                    \
+                 : "+v"(acc[0]), "+v"(acc[1])                                                \
+                 : "v"(a), "v"(b[0]), "v"(b[1]), "s"(which)                                  \
+                 : "scc")
+template <class Op>
+__device__ __forceinline__ void mfma_extra_tile_2(typename Op::Acc (&acc)[2], const i32x4& a, const i32x4 (&b)[2], int which) {
 #ifdef __HIP_DEVICE_COMPILE__
-#define MOE_ZM(J, B) "v_mfma_f32_16x16x32_bf16 %" #J ", %2, %" #B ", %" #J "\n\t"
-    asm volatile("s_cmp_lg_u32 %5, 0\n\ts_cbranch_scc1 1f\n\t"
-                 MOE_ZM(0, 3) MOE_ZM(1, 4)
-                 "s_branch 3f\n1:\n\ts_cmp_lg_u32 %5, 1\n\ts_cbranch_scc1 2f\n\t"
-                 MOE_ZM(0, 3)
-                 "s_branch 3f\n2:\n\t"
-                 MOE_ZM(1, 4)
-                 "3:\n\t"
-                 : "+v"(acc[0]), "+v"(acc[1])
-                 : "v"(a), "v"(b[0]), "v"(b[1]), "s"(which)
-                 : "scc");
+    if constexpr (Op::kScaled) MOE_EXTRA_2(MOE_MFMA_I8);
+    else MOE_EXTRA_2(MOE_MFMA_BF16);
 #endif
 }
 __device__ __forceinline__ void load_vgpr_16(i32x4& dst, const char* ptr) {
@@ -306,7 +292,7 @@ __device__ __forceinline__ void static_for(F&& f) {
 // chip and for the last round of a launch (see tail_tile).  0 (MODE 1): 256 rows x 64 columns, half of a page tile.  nt: column tile, in units of this block's columns.
 // TR: most rows of a row tile without its extra ones.  128 (the linear map with NB = 1): twice the blocks, none but the loops of
 // short tiles.
-template <int MODE, int NB, int TR>
+template <class Op, int MODE, int NB, int TR>
 __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& tc, const int nt) {
     static_assert((TR == BM || (TR == 128 && NB == 1)) && (NB > 0 || MODE == 1), "");
     constexpr int S = kStages;
@@ -427,9 +413,9 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
     const int extra_which = __builtin_amdgcn_readfirstlane(split_extra ? 1 + wm : 0);
     const char* ae_ptr = p.A;
     i32x4 AE[4];
-    f32x4 accE[NJ];
+    typename Op::Acc accE[NJ];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) accE[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NJ; ++j) accE[j] = typename Op::Acc{0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < 4; ++u) AE[u] = i32x4{0, 0, 0, 0};
     if (extra) {
@@ -507,17 +493,17 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
     };
     // accumulator tile (I, J) += a * b, alone or with a load behind it
     auto mfma = [&](auto i_c, auto j_c, const i32x4& a, const i32x4& b) __attribute__((always_inline)) {
-        mfma_16x16x32<(decltype(i_c)::value * NJ + decltype(j_c)::value) * 4>(a, b);
+        mfma_16x16<Op, (decltype(i_c)::value * NJ + decltype(j_c)::value) * 4>(a, b);
     };
     auto mfma_load_a = [&](auto i_c, auto j_c, const i32x4& a, const i32x4& b, auto ia_c) __attribute__((always_inline)) {   // + activation load instruction IA
         constexpr int IA = decltype(ia_c)::value;
-        mfma_16x16x32_then_load<(decltype(i_c)::value * NJ + decltype(j_c)::value) * 4, IA * kWaves * 1024, false>(a, b, a_ptr, a_off[IA], a_wr_w);
+        mfma_16x16_then_load<Op, (decltype(i_c)::value * NJ + decltype(j_c)::value) * 4, IA * kWaves * 1024, false>(a, b, a_ptr, a_off[IA], a_wr_w);
         advance_a(IA);
     };
     auto mfma_load_b = [&](auto i_c, auto j_c, const i32x4& a, const i32x4& b, auto slot_c, auto l_c, auto stream_c, int kn) __attribute__((always_inline)) {   // + weight load instruction L of half-step kn into slot SLOT
         constexpr int SLOT = decltype(slot_c)::value, I = decltype(l_c)::value;
         constexpr int odd = SLOT & 1;               // S is even: the parity of the half-step is that of its slot
-        mfma_16x16x32_then_load<(decltype(i_c)::value * NJ + decltype(j_c)::value) * 4, SLOT * kStageB + I * (kWaves * 1024), decltype(stream_c)::value>(
+        mfma_16x16_then_load<Op, (decltype(i_c)::value * NJ + decltype(j_c)::value) * 4, SLOT * kStageB + I * (kWaves * 1024), decltype(stream_c)::value>(
             a, b, (I < kPart / (kWaves * 1024) ? w0 : w1).tile, b_voff[odd][(I * (kWaves * 1024)) % kPart / (kWaves * 1024)], lds_wave);
         advance_b(kn, odd, I);
     };
@@ -619,9 +605,9 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
                     }
                 });
                 if constexpr (TALL) {                        // tall tile: the extra row tile against the column fragments of k
-                    if constexpr (NJ == 2) mfma_extra_tile_2(accE, AE[U], BF[HP], extra_which);
-                    else if constexpr (NJ == 8) mfma_extra_tile_8<MODE == 0>(accE, AE[U], BF[HP], extra_which);
-                    else mfma_extra_tile_4<MODE == 0>(accE, AE[U], BF[HP], extra_which);
+                    if constexpr (NJ == 2) mfma_extra_tile_2<Op>(accE, AE[U], BF[HP], extra_which);
+                    else if constexpr (NJ == 8) mfma_extra_tile_8<Op, MODE == 0>(accE, AE[U], BF[HP], extra_which);
+                    else mfma_extra_tile_4<Op, MODE == 0>(accE, AE[U], BF[HP], extra_which);
                     MOE_FENCE();
                     // the fragment of half-step k + 4: there is one exactly while the activation loads go on (the last four
                     // half-steps run without LA), so no test of k is needed
@@ -769,6 +755,33 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
     const int col_l = lane & 15;
     const int a_row_base = wm * (row_tiles > 4 ? 16 * row_tiles : 64) + (lane >> 4) * 4;
     const bool full_rows = rows_here >= BM;
+    // Integers: the scales of the tile's rows go through LDS (free now), those of the columns straight into registers.  Sum v of row `row` and fragment j
+    // is worth value(v, row, j).
+    float* const sw = (float*)smem;
+    float col_scale[Op::kScaled ? NJ : 1];
+    if constexpr (Op::kScaled) {
+        auto scale_of = [&](int row) __attribute__((always_inline)) {
+            const int64_t src = p.a_gather ? min(max(p.a_gather[row0 + row] / p.a_div, 0), p.a_rows - 1) : row0 + row;
+            float v = p.a_scale[src];
+            if (MODE == 1 && p.row_w) v *= p.row_w[row0 + row];
+            return v;
+        };
+        const float mine = scale_of(min(tid, rows_here - 1)), more = extra && tid < 32 ? scale_of(min(BM + tid, rows_here - 1)) : 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int c = MODE == 0 ? nt * (16 * NJ) + wn * (8 * NJ) + (j % (NJ / 2)) * 16 + col_l : min(nt * (32 * NJ) + wn * (16 * NJ) + j * 16 + col_l, p.n_cols - 1);
+            col_scale[j] = (MODE == 0 && j >= NJ / 2 ? p.w_scale_up : p.w_scale)[(int64_t)e * p.n_cols + c];
+        }
+        __syncthreads();                       // every wavefront has left the main loop
+        sw[tid] = mine;
+        if (tid < 32) sw[BM + tid] = more;     // a tall tile's extra rows
+        __syncthreads();
+    }
+    auto value = [&](auto sum, int row, int j) __attribute__((always_inline)) -> float {
+        if constexpr (!Op::kScaled) return sum;
+        else if constexpr (std::is_same<decltype(sum), float>::value) return (float)__float_as_int(sum) * col_scale[j] * sw[row];      // as read from an accumulator register
+        else return (float)sum * col_scale[j] * sw[row];
+    };
     // store(i, v): the 4 x NJ x 16 values of row tile i of this wavefront
     auto for_row_tiles = [&](auto n_c, auto&& store) __attribute__((always_inline)) {
         static_for<decltype(n_c)::value>([&](auto ic) __attribute__((always_inline)) {
@@ -801,7 +814,7 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
                     if (decltype(full)::value || row < rows_here) {
 #pragma unroll
                         for (int j = 0; j < NP; ++j)
-                            store_h(stream_c, (__bf16)silu_mul_bf16(v[j][r], v[j + NP][r]), h + (int64_t)row * p.ldo + j * 16);
+                            store_h(stream_c, (__bf16)silu_mul_bf16(value(v[j][r], row, j), value(v[j + NP][r], row, j + NP)), h + (int64_t)row * p.ldo + j * 16);
                     }
                 }
             });
@@ -825,21 +838,23 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
 #pragma unroll
                     for (int j = 0; j < NP; ++j)
                         if (!split_extra || j / (NP / 2) == wm)      // split: this wavefront row's gate fragments only
-                            h[(int64_t)row * p.ldo + j * 16] = (__bf16)silu_mul_bf16(accE[j][r], accE[j + NP][r]);
+                            h[(int64_t)row * p.ldo + j * 16] = (__bf16)silu_mul_bf16(value(accE[j][r], row, j), value(accE[j + NP][r], row, j + NP));
                 }
             }
         }
     } else {
         // the 256 row weights of the tile go through LDS (free now): one load per thread instead of
         // one dependent global load per accumulator row
-        float* sw = (float*)smem;
-        __syncthreads();                       // every wavefront has left the main loop
-        sw[tid] = (p.row_w && tid < rows_here) ? p.row_w[row0 + tid] : 1.0f;
-        if (tid < 32) sw[BM + tid] = (p.row_w && BM + tid < rows_here) ? p.row_w[row0 + BM + tid] : 1.0f;     // a tall tile's extra rows
-        __syncthreads();
+        if constexpr (!Op::kScaled) {
+            __syncthreads();                       // every wavefront has left the main loop
+            sw[tid] = (p.row_w && tid < rows_here) ? p.row_w[row0 + tid] : 1.0f;
+            if (tid < 32) sw[BM + tid] = (p.row_w && BM + tid < rows_here) ? p.row_w[row0 + BM + tid] : 1.0f;     // a tall tile's extra rows
+            __syncthreads();
+        }
         const int d0 = nt * (32 * NJ) + wn * (16 * NJ);   // n_cols is a multiple of 128: with NB = 2 a wavefront's columns are all valid or all not
         if (d0 < p.n_cols) {
-            float* o = (float*)p.out + (int64_t)row0 * p.ldo + d0 + col_l;
+            typedef typename Op::Out Out;
+            Out* o = (Out*)p.out + (int64_t)row0 * p.ldo + d0 + col_l;
             auto store_rows = [&](auto full, auto n_c) __attribute__((always_inline)) {
                 for_row_tiles(n_c, [&](int i, float (&v)[NJ][4]) __attribute__((always_inline)) {
                     const int rowq = a_row_base + i * 16;      // 4 consecutive rows
@@ -851,7 +866,7 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
                         if (decltype(full)::value || row < rows_here) {
 #pragma unroll
                             for (int j = 0; j < NJ; ++j)
-                                o[(int64_t)row * p.ldo + j * 16] = v[j][r] * w4[r];
+                                o[(int64_t)row * p.ldo + j * 16] = Op::kScaled ? (Out)((float)__float_as_int(v[j][r]) * col_scale[Op::kScaled ? j : 0] * w4[r]) : (Out)(v[j][r] * w4[r]);
                         }
                     }
                 });
@@ -871,7 +886,8 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
                         const float wr = sw[row];
 #pragma unroll
                         for (int j = 0; j < NJ; ++j)
-                            if (!split_extra || j / (NJ / 2) == wm) o[(int64_t)row * p.ldo + j * 16] = accE[j][r] * wr;      // split: this wavefront row's half
+                            if (!split_extra || j / (NJ / 2) == wm)      // split: this wavefront row's half
+                                o[(int64_t)row * p.ldo + j * 16] = Op::kScaled ? (Out)((float)accE[j][r] * col_scale[Op::kScaled ? j : 0] * wr) : (Out)(accE[j][r] * wr);
                     }
                 }
             }
@@ -885,8 +901,8 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
 }
 
 // SPLIT: the tiles of a last, at most half full round are computed as two each of half the columns (see tail_tile).
-template <int MODE, int NB, int TR, bool SPLIT>
-__global__ __launch_bounds__(kThreads) void ffn_gemm_bf16(const GemmParams p) {
+template <class Op, int MODE, int NB, int TR, bool SPLIT>
+__global__ __launch_bounds__(kThreads) void ffn_gemm(const GemmParams p) {
     static_assert(!SPLIT || NB == 2 || (NB == 1 && MODE == 1), "");
     // the short search: layer of 64 experts of 2048 x 1024, 777 tokens 199.7 / 193.5 us, 1024 x 2816, 350 tokens 53.0 / 50.8
     const TileCoord tc = !SPLIT && TR == BM && p.chunked == 0 && p.offsets ? locate_single_groups<TR>(p) : locate_tile<TR, SPLIT>(p);
@@ -895,24 +911,24 @@ __global__ __launch_bounds__(kThreads) void ffn_gemm_bf16(const GemmParams p) {
         if (tc.half >= 0) {
             const int nt = 2 * tc.nt + tc.half;
             if (MODE == 1 && NB == 2 && nt >= p.n_page_tiles) return; // the last tile of an odd number of page tiles
-            gemm_tile<MODE, NB - 1, TR>(p, tc, nt);
+            gemm_tile<Op, MODE, NB - 1, TR>(p, tc, nt);
             return;
         }
     }
-    gemm_tile<MODE, NB, TR>(p, tc, tc.nt);
+    gemm_tile<Op, MODE, NB, TR>(p, tc, tc.nt);
 }
 
-template <int MODE, int NB, int TR = BM, bool SPLIT = false>
+template <class Op, int MODE, int NB, int TR = BM, bool SPLIT = false>
 int launch_stages(const GemmParams& p, int R, int n_exp, hipStream_t st) {
     constexpr int lds = kLdsBytes;
     const int grid = !SPLIT && TR == BM && p.chunked == 0 && p.offsets ? rows_grid(p.NT, R, TR, n_exp) : gemm_grid(p.NT, R, TR, n_exp, p.chunked, SPLIT, p.balance && p.xcd_remap);
     static std::once_flag once;
     static hipError_t attr_err = hipSuccess;
     std::call_once(once, [] {
-        attr_err = hipFuncSetAttribute((const void*)ffn_gemm_bf16<MODE, NB, TR, SPLIT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        attr_err = hipFuncSetAttribute((const void*)ffn_gemm<Op, MODE, NB, TR, SPLIT>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     });
     MOE_HIP_TRY(attr_err);
-    hipLaunchKernelGGL((ffn_gemm_bf16<MODE, NB, TR, SPLIT>), dim3(grid), dim3(kThreads), lds, st, p);
+    hipLaunchKernelGGL((ffn_gemm<Op, MODE, NB, TR, SPLIT>), dim3(grid), dim3(kThreads), lds, st, p);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }

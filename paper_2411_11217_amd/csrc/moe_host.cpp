@@ -10,27 +10,41 @@
 
 namespace moe {
 
+constexpr int64_t kLinearTileBytes = 16384;      // of a bf16 and of an 8-bit tile
+
+static int esize_of(int dtype) { return dtype == MOE_DTYPE_F32 ? 4 : dtype == MOE_DTYPE_BF16 ? 2 : 1; }
+static int tile_k_of(int dtype) { return dtype == MOE_DTYPE_I8 ? kTileKI8 : kTileK; }
+// Reduction lengths of 8-bit integers: the loops take two tiles at a time, and 128 * 128 * k has to stay below 2^31.
+static bool takes_i8_length(int64_t k) { return k % (2 * kTileKI8) == 0 && k * 128 * 128 < ((int64_t)1 << 31); }
+
 int validate_shape(const moe_shape* s) {
     if (!s) return MOE_ERR_INVALID_ARG;
-    if (s->dtype != MOE_DTYPE_F32 && s->dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED_DTYPE;
+    if (s->dtype != MOE_DTYPE_F32 && s->dtype != MOE_DTYPE_BF16 && s->dtype != MOE_DTYPE_I8) return MOE_ERR_UNSUPPORTED_DTYPE;
     if (s->T < 0 || s->H <= 0 || s->F <= 0 || s->E < 1 || s->E > MOE_MAX_EXPERTS) return MOE_ERR_INVALID_ARG;
     if (s->k < 1 || s->k > s->E) return MOE_ERR_INVALID_ARG;
     if (s->H % kTileN != 0 || s->F % kTileN != 0) return MOE_ERR_INVALID_ARG;
+    if (s->dtype == MOE_DTYPE_I8 && (!takes_i8_length(s->H) || !takes_i8_length(s->F))) return MOE_ERR_INVALID_ARG;
     if ((int64_t)s->T * s->k > (int64_t)0x3fffffff) return MOE_ERR_INVALID_ARG;
-    const int64_t tile = (int64_t)kTileN * kTileK * (s->dtype == MOE_DTYPE_BF16 ? 2 : 4);
+    const int64_t tile = (int64_t)kTileN * tile_k_of(s->dtype) * esize_of(s->dtype);
     if (s->page_bytes <= 0 || s->page_bytes % tile != 0) return MOE_ERR_INVALID_ARG;
     return MOE_OK;
 }
 
+int validate_float_shape(const moe_shape* s) {
+    if (s && s->dtype == MOE_DTYPE_I8) return MOE_ERR_UNSUPPORTED_DTYPE;
+    return validate_shape(s);
+}
+
 Geom geometry(const moe_shape& s) {
     Geom g;
-    g.esize = s.dtype == MOE_DTYPE_BF16 ? 2 : 4;
-    g.tile_bytes = (int64_t)kTileN * kTileK * g.esize;
+    g.esize = esize_of(s.dtype);
+    g.tile_k = tile_k_of(s.dtype);
+    g.tile_bytes = (int64_t)kTileN * g.tile_k * g.esize;
     g.tpp = s.page_bytes / g.tile_bytes;
-    g.kt_gu = s.H / kTileK;
+    g.kt_gu = s.H / g.tile_k;
     g.ft = s.F / kTileN;
     g.tiles_gu = 2 * g.ft * g.kt_gu;
-    g.kt_d = s.F / kTileK;
+    g.kt_d = s.F / g.tile_k;
     g.dt = s.H / kTileN;
     g.tiles_d = g.dt * g.kt_d;
     g.pages_gu = (g.tiles_gu + g.tpp - 1) / g.tpp;
@@ -53,18 +67,18 @@ int validate_kv(const moe_kv_shape* s) {
 
 // ---- packer -------------------------------------------------------------------
 // Byte offset inside a page tile of the 16-byte chunk c of row n (the page format of moe.h).
-// bf16: two half-tiles of 128 rows x 64 bytes, chunk c & 3 of half c >> 2 at position
+// bf16 and 8-bit integers: two half-tiles of 128 rows x 64 bytes, chunk c & 3 of half c >> 2 at position
 // (c & 3) ^ ((n >> 2) & 2).  f32: 128 rows x 256 bytes, chunk c at position
 // (c & 8) | ((c & 7) ^ ((n >> 1) & 7)).
 static inline int64_t tile_chunk_offset(int esize, int n, int c) {
-    if (esize == 2) return (int64_t)(c >> 2) * (kTileN * 64) + n * 64 + (((c & 3) ^ ((n >> 2) & 2)) << 4);
+    if (esize <= 2) return (int64_t)(c >> 2) * (kTileN * 64) + n * 64 + (((c & 3) ^ ((n >> 2) & 2)) << 4);
     return (int64_t)n * (kTileK * 4) + (((c & 8) | ((c & 7) ^ ((n >> 1) & 7))) << 4);
 }
 
-// Copies one 128 x 64 tile between a dense row-major matrix (leading dimension
+// Copies one tile (128 rows) between a dense row-major matrix (leading dimension
 // ld elements) and its page image.  to_page: dense -> page, else page -> dense.
 void copy_tile(char* page_tile, char* dense, int64_t ld, int esize, bool to_page) {
-    const int chunks = kTileK * esize / 16;
+    const int chunks = (esize == 1 ? kTileKI8 : kTileK) * esize / 16;
     for (int n = 0; n < kTileN; ++n) {
         char* drow = dense + (int64_t)n * ld * esize;
         for (int c = 0; c < chunks; ++c) {
@@ -112,12 +126,12 @@ static int pack_or_unpack(const moe_shape* s, char* W1, char* W3, char* W2, cons
         for (int64_t f = 0; f < g.ft; ++f)
             for (int w = 0; w < 2; ++w)
                 for (int64_t kt = 0; kt < g.kt_gu; ++kt) {
-                    char* dense = (w == 0 ? W1 : W3) + (((int64_t)e * F + f * kTileN) * H + kt * kTileK) * g.esize;
+                    char* dense = (w == 0 ? W1 : W3) + (((int64_t)e * F + f * kTileN) * H + kt * g.tile_k) * g.esize;
                     copy_tile(tile_ptr(0, (f * 2 + w) * g.kt_gu + kt), dense, H, g.esize, to_page);
                 }
         for (int64_t d = 0; d < g.dt; ++d)
             for (int64_t kt = 0; kt < g.kt_d; ++kt) {
-                char* dense = W2 + (((int64_t)e * H + d * kTileN) * F + kt * kTileK) * g.esize;
+                char* dense = W2 + (((int64_t)e * H + d * kTileN) * F + kt * g.tile_k) * g.esize;
                 copy_tile(tile_ptr(g.pages_gu, d * g.kt_d + kt), dense, F, g.esize, to_page);
             }
     };
@@ -131,17 +145,22 @@ static int pack_or_unpack(const moe_shape* s, char* W1, char* W3, char* W2, cons
 
 int validate_linear(const moe_linear_shape* s) {
     if (!s) return MOE_ERR_INVALID_ARG;
-    if (s->dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED_DTYPE;
+    if (s->dtype != MOE_DTYPE_BF16 && s->dtype != MOE_DTYPE_I8) return MOE_ERR_UNSUPPORTED_DTYPE;
     if (s->T < 0 || s->K < 128 || s->N < 128 || s->K % 128 != 0 || s->N % kTileN != 0) return MOE_ERR_INVALID_ARG;
+    if (s->dtype == MOE_DTYPE_I8 && !takes_i8_length(s->K)) return MOE_ERR_INVALID_ARG;
     if ((int64_t)s->T > 0x3fffffff) return MOE_ERR_INVALID_ARG;
-    const int64_t tile = (int64_t)kTileN * kTileK * 2;
-    if (s->page_bytes <= 0 || s->page_bytes % tile != 0) return MOE_ERR_INVALID_ARG;
+    if (s->page_bytes <= 0 || s->page_bytes % kLinearTileBytes != 0) return MOE_ERR_INVALID_ARG;
     return MOE_OK;
 }
 
+int validate_bf16_linear(const moe_linear_shape* s) {
+    if (s && s->dtype == MOE_DTYPE_I8) return MOE_ERR_UNSUPPORTED_DTYPE;
+    return validate_linear(s);
+}
+
 int64_t linear_pages(const moe_linear_shape& s) {
-    const int64_t tiles = (int64_t)(s.N / kTileN) * (s.K / kTileK);
-    const int64_t tpp = s.page_bytes / ((int64_t)kTileN * kTileK * 2);
+    const int64_t tiles = (int64_t)(s.N / kTileN) * (s.K / tile_k_of(s.dtype));
+    const int64_t tpp = s.page_bytes / kLinearTileBytes;
     return (tiles + tpp - 1) / tpp;
 }
 
@@ -215,7 +234,7 @@ int moe_linear_pack(const moe_linear_shape* s, const void* W, const int32_t* pag
     int rc = validate_linear(s);
     if (rc != MOE_OK) return rc;
     if (!W || !page_table || !pages_out || pool_pages <= 0) return MOE_ERR_INVALID_ARG;
-    const int64_t n_pages = linear_pages(*s), tile_bytes = (int64_t)kTileN * kTileK * 2, tpp = s->page_bytes / tile_bytes;
+    const int64_t n_pages = linear_pages(*s), tile_bytes = kLinearTileBytes, tpp = s->page_bytes / tile_bytes;
     std::vector<char> seen((size_t)pool_pages, 0);
     for (int64_t p = 0; p < n_pages; ++p) {
         const int32_t v = page_table[p];
@@ -223,14 +242,15 @@ int moe_linear_pack(const moe_linear_shape* s, const void* W, const int32_t* pag
         if (seen[(size_t)v]) return MOE_ERR_INVALID_ARG;
         seen[(size_t)v] = 1;
     }
-    const int64_t kt_n = s->K / kTileK, nt_n = s->N / kTileN, tiles = kt_n * nt_n;
+    const int esize = esize_of(s->dtype), tile_k = tile_k_of(s->dtype);
+    const int64_t kt_n = s->K / tile_k, nt_n = s->N / kTileN, tiles = kt_n * nt_n;
     auto tile_ptr = [&](int64_t ti) {
         return (char*)pages_out + (int64_t)page_table[ti / tpp] * s->page_bytes + (ti % tpp) * tile_bytes;
     };
     for (int64_t ti = tiles; ti < n_pages * tpp; ++ti) std::memset(tile_ptr(ti), 0, (size_t)tile_bytes);   // padding of the last page
     for (int64_t nt = 0; nt < nt_n; ++nt)
         for (int64_t kt = 0; kt < kt_n; ++kt)
-            copy_tile(tile_ptr(nt * kt_n + kt), (char*)W + ((nt * kTileN) * (int64_t)s->K + kt * kTileK) * 2, s->K, 2, true);
+            copy_tile(tile_ptr(nt * kt_n + kt), (char*)W + ((nt * kTileN) * (int64_t)s->K + kt * tile_k) * esize, s->K, esize, true);
     return MOE_OK;
 }
 

@@ -8,33 +8,36 @@
 
 namespace moe {
 
-// Weight tile: 128 output features x 64 reduction elements (see the page
-// format in moe.h).  A bf16 tile is stored as two half-tiles of 32 reduction
+// Weight tile: 128 output features x 64 reduction elements, of 8-bit integers 128 (see the page
+// format in moe.h).  A bf16 or 8-bit tile is stored as two half-tiles of half of its reduction
 // elements each.
 constexpr int kTileN = 128;
 constexpr int kTileK = 64;
+constexpr int kTileKI8 = 128;
 
 struct Geom {
     int esize;            // bytes per element of dtype
-    int64_t tile_bytes;   // kTileN * kTileK * esize
+    int tile_k;           // reduction elements of a tile: kTileK or kTileKI8
+    int64_t tile_bytes;   // kTileN * tile_k * esize
     int64_t tpp;          // tiles per page
-    int64_t kt_gu;        // H / 64  : k-tiles of the gate/up product
+    int64_t kt_gu;        // H / tile_k : k-tiles of the gate/up product
     int64_t ft;           // F / 128 : f-tiles (each has a W1 and a W3 tile row)
     int64_t tiles_gu;     // 2 * ft * kt_gu
-    int64_t kt_d;         // F / 64  : k-tiles of the down product
+    int64_t kt_d;         // F / tile_k : k-tiles of the down product
     int64_t dt;           // H / 128 : d-tiles
     int64_t tiles_d;      // dt * kt_d
     int64_t pages_gu, pages_d, ppe;   // pages per expert: GU group, D group, both
 };
 
 int validate_shape(const moe_shape* s);          // MOE_OK or error
+int validate_float_shape(const moe_shape* s);    // the same, for the calls that do not take 8-bit integers
 Geom geometry(const moe_shape& s);               // shape must be valid
 
 // MOE_OK, MOE_ERR_PAGE_NOT_RESIDENT (an entry outside [0, pool_pages)) or, with need_distinct,
 // MOE_ERR_INVALID_ARG when two entries name the same slot.  table: host int32[E][ppe].
 int check_table_host(const moe_shape& s, const Geom& g, const int32_t* table, int64_t pool_pages, bool need_distinct);
 
-// Copies one 128 x 64 weight tile between a dense row-major matrix (leading dimension ld elements)
+// Copies one weight tile (128 rows) between a dense row-major matrix (leading dimension ld elements)
 // and its page image.
 void copy_tile(char* page_tile, char* dense, int64_t ld, int esize, bool to_page);
 
@@ -45,7 +48,8 @@ inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
 }
 
 // Dense paged matrices (moe_linear): MOE_OK or an error; pages of one matrix (shape must be valid).
-int validate_linear(const moe_linear_shape* s);
+int validate_linear(const moe_linear_shape* s);              // bf16 or 8-bit integers
+int validate_bf16_linear(const moe_linear_shape* s);
 int64_t linear_pages(const moe_linear_shape& s);
 
 // Attention over a paged cache: MOE_OK or an error.
@@ -62,10 +66,10 @@ inline uint64_t division_magic(int32_t d, int& shift) {
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Where the dense linear map takes the kernel for few rows (csrc/moe_ffn_rows_bf16.hip): as long as blocks of 64 columns and 128
+// Where the dense linear map takes the kernel for few rows (csrc/moe_ffn_rows.h): as long as blocks of 64 columns and 128
 // rows, or with more than 128 rows of 128 columns and 64 rows, make one round on the 256 compute units (which blocks it has
 // then is linear_rows_block's choice), and with a short k and few rows.
-//   One matrix alone has too few columns to fill the chip with 256-row blocks (moe_ffn_gemm_bf16.h).  us, those blocks / this
+//   One matrix alone has too few columns to fill the chip with 256-row blocks (moe_ffn_gemm.h).  us, those blocks / this
 // kernel, weights where the call before left them | weights from HBM (copies that exceed the last-level cache in turn): 4096 x
 // 6144 (K x N) 1 token - | 45 / 15, 100: - | 47 / 30; 6144 x 9216 16 tokens 33 / 21 | 48 / 29, 100: 41 / 39 | 59 / 50;
 // 4096 x 16384 (one full round) 16 tokens 25 / 22 | 42 / 27, 64: 31 / 24 | 40 / 30, 128: 32 / 32 | 46 / 42; 8192 x 1024 600

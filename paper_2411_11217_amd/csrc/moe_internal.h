@@ -86,10 +86,46 @@ struct LinearArgs {
     uint16_t* out16;           // bf16 [T][N] or null: out rounded to nearest even as well
     int32_t* status;           // [4] or null
 };
+
+// ---- 8-bit integers
+struct LinearI8Args {
+    const int8_t* x;           // [T][K]
+    const float* x_scale;      // [T]
+    int T, K, N;
+    const int32_t* page_table;
+    const char* pool;
+    int64_t pool_pages, page_bytes, pages;
+    const float* w_scale;      // [N]
+    float* out;                // [T][N]
+    int32_t* status;           // [4] or null
+};
+int launch_linear_i8(const LinearI8Args& a, hipStream_t st);
+struct FfnI8Args {
+    const int8_t* x;           // [R][H], or with row_src [T][H]
+    const float* x_scale;
+    const int32_t* row_src;    // null, or row r reads x[row_src[r] / k]
+    const int32_t* offsets;
+    const int32_t* page_table;
+    const char* pool;
+    int64_t pool_pages;
+    moe_expert_scales scales;
+    const float* row_w;        // [R] or null
+    void* h;                   // bf16 [R][F]
+    int8_t* h_q;               // [R][F]
+    float* h_scale;            // [R]
+    void* out;                 // bf16 [R][H]
+    int32_t* status;
+};
+int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st);
+int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, hipStream_t st);
+bool norm_takes(int32_t H, float eps);
+int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* q, float* scale,
+                          hipStream_t st);
+
 int launch_cast_bf16(int64_t n, const float* in, void* out, hipStream_t st);
 int launch_linear_bf16(const LinearArgs& a, hipStream_t st);
 
-int launch_combine(const moe_shape& s, const float* out, const int32_t* row_of, const float* topk_w,
+int launch_combine(const moe_shape& s, const void* out, const int32_t* row_of, const float* topk_w,
                    float* y, hipStream_t st);
 
 }  // namespace moe

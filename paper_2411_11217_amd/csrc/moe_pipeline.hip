@@ -62,7 +62,7 @@ int enqueue_chunk(moe_pipeline* p, int layer, int half, int64_t first, int64_t l
 extern "C" {
 
 int moe_pipeline_pool_pages(const moe_shape* s, int32_t n_layers, int32_t resident_pages_per_expert, int64_t* pool_pages) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     const Geom g = geometry(*s);
     if (!pool_pages || n_layers < 1 || resident_pages_per_expert < 0 || resident_pages_per_expert > g.ppe)
@@ -76,7 +76,7 @@ int moe_pipeline_create(const moe_shape* s, int32_t n_layers, int32_t max_micro_
                         const int32_t* const* host_page_tables, int32_t resident_pages_per_expert,
                         void* device_pool, int64_t device_pool_pages, int32_t* device_tables,
                         moe_pipeline** out) {
-    int rc = validate_shape(s);
+    int rc = validate_float_shape(s);
     if (rc != MOE_OK) return rc;
     const Geom g = geometry(*s);
     if (n_layers < 1 || max_micro_batches < 1 || !host_pages || !host_pool_pages || !host_page_tables || !device_pool ||

@@ -239,7 +239,7 @@ inline int gemm_grid(int NT, int R, int BM, int n_experts, int chunked, bool spl
     return (int)(8 * (plain_groups * M + slack * n_experts + (split ? 16 : 0)));
 }
 
-// The order of the kernel for few rows per expert (moe_ffn_rows_bf16.hip).  Its tiles are numbered expert by expert, inside an
+// The order of the kernel for few rows per expert (moe_ffn_rows.h).  Its tiles are numbered expert by expert, inside an
 // expert of m row tiles in runs of eight column tiles, the row tiles of a run one after the other.  Block b runs on XCD b % 8:
 // in a run of eight the row tiles of a column tile meet in one L2, in a last run of fewer columns they do not.
 // -> row tile and column tile of tile number rel (0 <= rel < m * NT) of the expert.
