@@ -17,7 +17,7 @@ int launch_expert_ffn_bf16(const moe_shape& s, const Geom& g, const FfnArgs& a, 
         if (rc != MOE_OK) return rc;
         if (a.mid_event) MOE_HIP_TRY(hipEventRecord(a.mid_event, st));
         fill_down(p, s, g, a);
-        return thin_takes_down(s) ? launch_down_thin_bf16(p, s.H, R, n_exp, st) : launch_down_rows_bf16(p, s.H, R, (int)rows_each, n_exp, st);
+        return thin_takes_down(s, s.F) ? launch_down_thin_bf16(p, s.H, R, n_exp, st) : launch_down_rows_bf16(p, s.H, R, (int)rows_each, n_exp, st);
     }
     const int64_t row_tiles_each = std::max<int64_t>(1, (rows_each - p.tall_rows + BM - 1) / BM);
     // A last round that is at most half full, by the tiles that an even split of the rows over the experts would give: its tiles are

@@ -265,15 +265,27 @@ __device__ __forceinline__ float silu_mul_bf16(float g, float u) {
 }
 
 // the kernel for few rows per expert (moe_ffn_rows.h); p as filled for the launch, NT is set there
-bool rows_kernel_takes(int rows_each);
+constexpr int kRowsKernelMax = 80;                   // rows per expert on average; measured in moe_ffn_rows.h
+inline bool rows_kernel_takes(int rows_each) { return rows_each <= kRowsKernelMax; }
 int launch_gate_up_rows_bf16(GemmParams& p, int F, int R, int rows_each, int n_exp, hipStream_t st);
 int launch_down_rows_bf16(GemmParams& p, int H, int R, int rows_each, int n_exp, hipStream_t st);
 int launch_linear_rows_bf16(GemmParams& p, int N, int T, hipStream_t st);
-// the one for a handful of tokens (moe_ffn_thin.h)
+// the one for a handful of tokens (moe_ffn_thin.h); k: its reduction elements if they were bf16, F or of 8-bit integers F / 2
 bool thin_takes_gate_up(const moe_shape& s);
-bool thin_takes_down(const moe_shape& s);
+bool thin_takes_down(const moe_shape& s, int k);
 int launch_gate_up_thin_bf16(GemmParams& p, int F, int R, int n_exp, hipStream_t st);
 int launch_down_thin_bf16(GemmParams& p, int H, int R, int n_exp, hipStream_t st);
+
+// the launches of the 256-row blocks (moe_ffn_gemm.h) with 8-bit integers: gate/up and down whole or with their last round in halves, the
+// down launch with 128-wide column tiles, whole or 64-wide in the last round; the linear map
+int launch_gate_up_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
+int launch_gate_up_halves_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
+int launch_down_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
+int launch_down_halves_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
+int launch_down_narrow_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
+int launch_down_narrow_halves_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
+int launch_linear_wide_i8(const GemmParams& p, int T, hipStream_t st);
+int launch_linear_narrow_i8(const GemmParams& p, int rows, int T, hipStream_t st);
 
 // the bf16 launches whose last round of tiles is computed in halves (moe_ffn_halves_bf16.hip)
 int launch_gate_up_halves_bf16(const GemmParams& p, int R, int n_exp, hipStream_t st);
@@ -296,7 +308,7 @@ inline void fill_common(GemmParams& p, const moe_shape& s, const Geom& g, const 
     p.status = a.status;
     p.xcd_remap = get_opt(OPT_XCD_REMAP);
     p.half_tiles = get_opt(OPT_HALF_TILES);
-    p.tall_rows = (s.dtype == MOE_DTYPE_BF16 && get_opt(OPT_TALL_TILES)) ? 32 : 0;
+    p.tall_rows = (s.dtype != MOE_DTYPE_F32 && get_opt(OPT_TALL_TILES)) ? 32 : 0;
     p.tall_first = get_opt(OPT_TALL_FIRST);
     p.balance = get_opt(OPT_BALANCE);
     // chunks only when the experts have more than half a row tile of rows on average: below that the launch streams

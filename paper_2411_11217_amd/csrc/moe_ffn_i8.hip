@@ -6,15 +6,21 @@
 // h is rounded to bf16 on its way to the 8 bits, as the bf16 layer's is: its scale is known only when all column tiles of its row are done, and as
 // float32 the way there and back would cost twice the bytes.  The step of the 8 bits is max |h| / 127; bf16 is off by |h| / 512 at most, a quarter of
 // that step for the largest values and less for all others.
+//
+// Kernels, tiles and pages count bytes along k (moe_ffn_op.h), so a launch over k integers is the launch over k / 2 bf16 in its loads, its MFMAs and their
+// times, and the rules measured for those hold with k / 2 in the place of k.
 #include "moe_ffn_rows.h"
+#include "moe_ffn_thin.h"
 
 namespace moe {
 
 typedef Int8<float> ToFloat;
 typedef Int8<__bf16> ToBf16;
+constexpr int kUnits = 256;                  // compute units
+constexpr int kTileRows = 256;               // of the blocks of moe_ffn_gemm.h
 
 int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st) {
-    const int R = s.T * s.k;
+    const int R = s.T * s.k, rows_each = R / s.E;
     const Geom g = geometry(s);
     FfnArgs f{};
     f.x_perm = a.x;
@@ -33,7 +39,17 @@ int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st)
     p.a_scale = a.x_scale;
     p.w_scale = a.scales.w1;
     p.w_scale_up = a.scales.w3;
-    int rc = launch_rows<ToFloat, 0, 8, 8, 1, 1, 2>(p, s.F, R, s.E, st);
+    // as launch_expert_ffn_bf16 (moe_ffn_bf16.hip)
+    const bool streams = rows_each <= 256 && (int64_t)s.E * 3 * s.H * s.F > ((int64_t)256 << 20);
+    p.stream = !streams ? 0 : s.F >= 6144 && s.E * g.dt >= kUnits ? 2 : 1;
+    const bool few = rows_kernel_takes(rows_each);
+    const int64_t row_tiles_each = std::max<int64_t>(1, (rows_each - p.tall_rows + kTileRows - 1) / kTileRows);
+    auto half_round = [&]() {
+        const int64_t last = s.E * row_tiles_each * p.NT % kUnits;
+        return last != 0 && last <= kUnits / 2;
+    };
+    int rc = !few ? (half_round() ? launch_gate_up_halves_i8(p, R, s.E, st) : launch_gate_up_i8(p, R, s.E, st))
+             : thin_takes_gate_up(s) ? launch_thin<ToFloat, 0, 2>(p, s.F, R, s.E, st) : gate_up_rows<ToFloat>(p, s.F, R, rows_each, s.E, st);
     if (rc != MOE_OK) return rc;
     rc = launch_quantize_i8(R, s.F, a.h, MOE_DTYPE_BF16, s.F, a.h_q, a.h_scale, st);
     if (rc != MOE_OK) return rc;
@@ -42,7 +58,14 @@ int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st)
     p.a_scale = a.h_scale;
     p.w_scale = a.scales.w2;
     p.row_w = a.row_w;
-    return launch_rows<ToBf16, 1, 8, 8, 1, 1, 4>(p, s.H, R, s.E, st);
+    if (few) return thin_takes_down(s, s.F / 2) ? launch_thin<ToBf16, 1, 1>(p, s.H, R, s.E, st) : down_rows<ToBf16>(p, s.H, R, rows_each, s.E, st);
+    const int opt = get_opt(OPT_DOWN_COLS);
+    const int64_t narrow_tiles = s.E * row_tiles_each * g.dt;
+    if (opt == 1 || (opt == 0 && narrow_tiles <= kUnits)) {
+        p.NT = (int32_t)g.dt;
+        return narrow_tiles <= kUnits / 2 ? launch_down_narrow_halves_i8(p, R, s.E, st) : launch_down_narrow_i8(p, R, s.E, st);
+    }
+    return half_round() ? launch_down_halves_i8(p, R, s.E, st) : launch_down_i8(p, R, s.E, st);
 }
 
 int launch_linear_i8(const LinearI8Args& a, hipStream_t st) {
@@ -66,7 +89,24 @@ int launch_linear_i8(const LinearI8Args& a, hipStream_t st) {
     p.status = a.status;
     p.a_scale = a.x_scale;
     p.w_scale = a.w_scale;
-    return launch_rows<ToFloat, 1, 4, 4, 1, 1, 4>(p, a.N, a.T, 1, st);
+    p.xcd_remap = get_opt(OPT_XCD_REMAP);
+    p.half_tiles = get_opt(OPT_HALF_TILES);
+    p.tall_rows = get_opt(OPT_TALL_TILES) ? 32 : 0;
+    p.tall_first = get_opt(OPT_TALL_FIRST);
+    p.balance = get_opt(OPT_BALANCE);
+    p.chunked = std::min(std::max(get_opt(OPT_CHUNKED), 0), 32);
+    // as launch_linear_bf16 (moe_ffn_bf16.hip)
+    if (linear_takes_rows_kernel(a.T, a.K / 2, a.N)) return linear_rows<ToFloat>(p, a.N, a.T, st);
+    const int wide_tiles = (p.n_page_tiles + 1) / 2;
+    if ((int64_t)(a.T / kTileRows + 1) * wide_tiles >= 2 * kUnits) {
+        p.NT = wide_tiles;
+        return launch_linear_wide_i8(p, a.T, st);
+    }
+    p.NT = p.n_page_tiles;
+    const int64_t half_tiles = (int64_t)((a.T + 127) / 128) * p.NT;
+    const bool low = p.half_tiles && a.T > 128 && half_tiles <= kUnits && (a.T > 160 || half_tiles <= 224 || p.KT <= 32);
+    if (low) p.tall_rows = 0;
+    return launch_linear_narrow_i8(p, low ? 128 : kTileRows, a.T, st);
 }
 
 }  // namespace moe

@@ -10,6 +10,9 @@ namespace moe {
 typedef int i32x4 __attribute__((ext_vector_type(4)));        // an MFMA operand: 16 bytes of a row
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kHalfTileBytes = 128 * 64;                     // half of a page tile's k: 32 bf16 or 64 integers of each row
+constexpr int kTileBytes = 2 * kHalfTileBytes;
+
 struct Bf16 {                                                 // v_mfma_f32_16x16x32_bf16: sums in float32
     static constexpr bool kScaled = false;
     typedef f32x4 Acc;

@@ -18,8 +18,6 @@
 namespace moe {
 namespace {
 
-constexpr int kHalfTileBytes = 128 * 64;             // 32 k of a page tile
-constexpr int kTileBytes = 2 * kHalfTileBytes;
 
 // CW: wavefronts of a block, side by side along the columns
 template <class Op, int MODE, int CW>

@@ -29,13 +29,13 @@ bool thin_takes_gate_up(const moe_shape& s) { return s.T <= 16 && experts_with_r
 // The routing is not known here.  The lower range goes by the average; the upper one by the average plus the deviation, or all experts, and where
 // k is not long by the average less half the deviation (routings that fill one round or less lose as much there as the others gain; with a long
 // k they lose little: 6144 x 16384, 8 experts, 4 tokens, 262 blocks on average, layer 522 / 502 over sixteen routings).
-bool thin_takes_down(const moe_shape& s) {
+bool thin_takes_down(const moe_shape& s, int k) {
     if (s.T > 16) return false;
     const double per_expert = s.H / 128;
     double deviation;
     const double blocks = experts_with_rows(s, &deviation) * per_expert;
-    if (s.F <= 2048) return blocks < 190 || (blocks > 256 && blocks < 500);
-    const bool long_k = s.F > 10240;
+    if (k <= 2048) return blocks < 190 || (blocks > 256 && blocks < 500);
+    const bool long_k = k > 10240;
     if (blocks < (long_k ? 190 : 130)) return true;
     return blocks - (long_k ? 0.0 : 0.5 * deviation * per_expert) > 256 && std::min(blocks + deviation * per_expert, s.E * per_expert) <= 384;
 }
