@@ -264,6 +264,15 @@ __device__ __forceinline__ float silu_mul_bf16(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
 }
 
+// The same for 8-bit integers, whose sums a (gate) and b (up) are still whole numbers: gate_scale and up_scale are the columns' scales times kGateFactor and
+// kUpFactor, which leaves the product as it is, (-g log2 e) (-u ln 2) = g u, and saves the multiplication by -log2 e.  All kernels form h this way, in this order, so
+// that a row has the same bits in each of them.
+constexpr float kGateFactor = -1.44269504088896340736f, kUpFactor = -0.69314718055994530942f;
+__device__ __forceinline__ float silu_mul_i8(int a, int b, float gate_scale, float up_scale, float row_scale) {
+    const float t = (float)a * gate_scale * row_scale, u = (float)b * up_scale * row_scale;
+    return t * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t)) * u;
+}
+
 // the kernel for few rows per expert (moe_ffn_rows.h); p as filled for the launch, NT is set there
 constexpr int kRowsKernelMax = 80;                   // rows per expert on average; measured in moe_ffn_rows.h
 inline bool rows_kernel_takes(int rows_each) { return rows_each <= kRowsKernelMax; }

@@ -76,6 +76,9 @@ namespace {
 
 #define MOE_FENCE() __builtin_amdgcn_sched_barrier(0)
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 typedef __attribute__((address_space(1))) const void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
@@ -321,8 +324,9 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
     // looks up the source of the wavefront's row (L / 8 * 4 + wave) * 8 + L % 8 here (one division per lane,
     // the load under way during the page-table lookups).
     uint32_t gathered = 0;
+    const int my_row = ((lane >> 3) * kWaves + wave) * 8 + (lane & 7);
     if (p.a_gather) {
-        const int r = min(((lane >> 3) * kWaves + wave) * 8 + (lane & 7), rows_here - 1);     // row0 + r is a row of this expert
+        const int r = min(my_row, rows_here - 1);     // row0 + r is a row of this expert
         gathered = (uint32_t)min(max(p.a_gather[row0 + r] / p.a_div, 0), p.a_rows - 1);      // clamped into the matrix at A
     }
 
@@ -422,6 +426,23 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
         const int er = min(BM + (split_extra ? 0 : wm * 16) + (lane & 15), rows_here - 1);
         const int64_t src = p.a_gather ? (int64_t)min(max(p.a_gather[row0 + er] / p.a_div, 0), p.a_rows - 1) : (int64_t)row0 + er;
         ae_ptr = p.A + src * p.lda_bytes + (lane >> 4) * 16;      // + 64 bytes per half-step
+    }
+    // Integers: the scales of row my_row, of a tall tile's extra row BM + tid and of this lane's columns, on their way before the operands and wanted after the main
+    // loop (looked up there they cost two memory latencies per tile, 2 of a gate/up tile's 98 k cycles).
+    float row_scale[2] = {0.f, 0.f}, row_weight[2] = {1.f, 1.f}, col_scale[Op::kScaled ? NJ : 1];
+    if constexpr (Op::kScaled) {
+        const int r = min(my_row, rows_here - 1), er = min(BM + tid, rows_here - 1);
+        row_scale[0] = p.a_scale[p.a_gather ? (int64_t)gathered : (int64_t)row0 + r];
+        if (MODE == 1 && p.row_w) row_weight[0] = p.row_w[row0 + r];
+        if (extra && tid < 32) {
+            row_scale[1] = p.a_scale[p.a_gather ? (int64_t)min(max(p.a_gather[row0 + er] / p.a_div, 0), p.a_rows - 1) : (int64_t)row0 + er];
+            if (MODE == 1 && p.row_w) row_weight[1] = p.row_w[row0 + er];
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int c = MODE == 0 ? nt * (16 * NJ) + wn * (8 * NJ) + (j % (NJ / 2)) * 16 + (lane & 15) : min(nt * (32 * NJ) + wn * (16 * NJ) + j * 16 + (lane & 15), p.n_cols - 1);
+            col_scale[j] = (MODE == 0 && j >= NJ / 2 ? p.w_scale_up : p.w_scale)[(int64_t)e * p.n_cols + c];
+        }
     }
     // weight half-tiles are copied linearly (HALVES: 64 rows of each)
     const uint32_t b_off = (HALVES ? (nt & 1) * kPart : 0) + wave * 1024 + lane * 16;
@@ -755,32 +776,20 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
     const int col_l = lane & 15;
     const int a_row_base = wm * (row_tiles > 4 ? 16 * row_tiles : 64) + (lane >> 4) * 4;
     const bool full_rows = rows_here >= BM;
-    // Integers: the scales of the tile's rows go through LDS (free now), those of the columns straight into registers.  Sum v of row `row` and fragment j
-    // is worth value(v, row, j).
+    // the scales of the tile's rows go through LDS (free now); sum v as an integer is bits(v)
     float* const sw = (float*)smem;
-    float col_scale[Op::kScaled ? NJ : 1];
     if constexpr (Op::kScaled) {
-        auto scale_of = [&](int row) __attribute__((always_inline)) {
-            const int64_t src = p.a_gather ? min(max(p.a_gather[row0 + row] / p.a_div, 0), p.a_rows - 1) : row0 + row;
-            float v = p.a_scale[src];
-            if (MODE == 1 && p.row_w) v *= p.row_w[row0 + row];
-            return v;
-        };
-        const float mine = scale_of(min(tid, rows_here - 1)), more = extra && tid < 32 ? scale_of(min(BM + tid, rows_here - 1)) : 0.f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int c = MODE == 0 ? nt * (16 * NJ) + wn * (8 * NJ) + (j % (NJ / 2)) * 16 + col_l : min(nt * (32 * NJ) + wn * (16 * NJ) + j * 16 + col_l, p.n_cols - 1);
-            col_scale[j] = (MODE == 0 && j >= NJ / 2 ? p.w_scale_up : p.w_scale)[(int64_t)e * p.n_cols + c];
-        }
         __syncthreads();                       // every wavefront has left the main loop
-        sw[tid] = mine;
-        if (tid < 32) sw[BM + tid] = more;     // a tall tile's extra rows
+        sw[my_row] = row_scale[0] * row_weight[0];
+        if (tid < 32) sw[BM + tid] = row_scale[1] * row_weight[1];     // a tall tile's extra rows
+        if (MODE == 0)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) col_scale[Op::kScaled ? j : 0] *= j < NJ / 2 ? kGateFactor : kUpFactor;
         __syncthreads();
     }
-    auto value = [&](auto sum, int row, int j) __attribute__((always_inline)) -> float {
-        if constexpr (!Op::kScaled) return sum;
-        else if constexpr (std::is_same<decltype(sum), float>::value) return (float)__float_as_int(sum) * col_scale[j] * sw[row];      // as read from an accumulator register
-        else return (float)sum * col_scale[j] * sw[row];
+    auto bits = [](auto v) __attribute__((always_inline)) -> int {
+        if constexpr (std::is_same<decltype(v), float>::value) return __float_as_int(v);
+        else return v;
     };
     // store(i, v): the 4 x NJ x 16 values of row tile i of this wavefront
     auto for_row_tiles = [&](auto n_c, auto&& store) __attribute__((always_inline)) {
@@ -808,13 +817,34 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
         };
         auto store_rows = [&](auto stream_c, auto full, auto n_c) __attribute__((always_inline)) {
             for_row_tiles(n_c, [&](int i, float (&v)[NJ][4]) __attribute__((always_inline)) {
+                if constexpr (Op::kScaled) {
+                    const int rowq = a_row_base + i * 16;      // 4 consecutive rows
+                    const f32x4 w4 = *(const f32x4*)(sw + rowq);
+#pragma unroll
+                    for (int r = 0; r < 4; r += 2) {           // two rows rounded by one instruction
+                        bf16x2 two[NP];
+#pragma unroll
+                        for (int j = 0; j < NP; ++j) {
+                            const f32x2 y{silu_mul_i8(bits(v[j][r]), bits(v[j + NP][r]), col_scale[j], col_scale[j + NP], w4[r]),
+                                          silu_mul_i8(bits(v[j][r + 1]), bits(v[j + NP][r + 1]), col_scale[j], col_scale[j + NP], w4[r + 1])};
+                            two[j] = __builtin_convertvector(y, bf16x2);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            if (decltype(full)::value || rowq + r + q < rows_here) {
+#pragma unroll
+                                for (int j = 0; j < NP; ++j) store_h(stream_c, two[j][q], h + (int64_t)(rowq + r + q) * p.ldo + j * 16);
+                            }
+                    }
+                    return;
+                }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = a_row_base + i * 16 + r;
                     if (decltype(full)::value || row < rows_here) {
 #pragma unroll
                         for (int j = 0; j < NP; ++j)
-                            store_h(stream_c, (__bf16)silu_mul_bf16(value(v[j][r], row, j), value(v[j + NP][r], row, j + NP)), h + (int64_t)row * p.ldo + j * 16);
+                            store_h(stream_c, (__bf16)silu_mul_bf16(v[j][r], v[j + NP][r]), h + (int64_t)row * p.ldo + j * 16);
                     }
                 }
             });
@@ -838,7 +868,8 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
 #pragma unroll
                     for (int j = 0; j < NP; ++j)
                         if (!split_extra || j / (NP / 2) == wm)      // split: this wavefront row's gate fragments only
-                            h[(int64_t)row * p.ldo + j * 16] = (__bf16)silu_mul_bf16(value(accE[j][r], row, j), value(accE[j + NP][r], row, j + NP));
+                            h[(int64_t)row * p.ldo + j * 16] = (__bf16)(Op::kScaled ? silu_mul_i8(bits(accE[j][r]), bits(accE[j + NP][r]), col_scale[Op::kScaled ? j : 0], col_scale[Op::kScaled ? j + NP : 0], sw[row])
+                                                                                    : silu_mul_bf16(accE[j][r], accE[j + NP][r]));
                 }
             }
         }
@@ -860,13 +891,27 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
                     const int rowq = a_row_base + i * 16;      // 4 consecutive rows
                     const float4 wq = *(const float4*)(sw + rowq);
                     const float w4[4] = {wq.x, wq.y, wq.z, wq.w};
+                    if constexpr (Op::kScaled) {
+#pragma unroll
+                        for (int r = 0; r < 4; r += 2)
+#pragma unroll
+                            for (int j = 0; j < NJ; ++j) {
+                                const f32x2 y{(float)bits(v[j][r]) * col_scale[j] * w4[r], (float)bits(v[j][r + 1]) * col_scale[j] * w4[r + 1]};
+                                typedef Out out2 __attribute__((ext_vector_type(2)));
+                                const out2 two = __builtin_convertvector(y, out2);       // two rows rounded by one instruction
+#pragma unroll
+                                for (int q = 0; q < 2; ++q)
+                                    if (decltype(full)::value || rowq + r + q < rows_here) o[(int64_t)(rowq + r + q) * p.ldo + j * 16] = two[q];
+                            }
+                        return;
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int row = rowq + r;
                         if (decltype(full)::value || row < rows_here) {
 #pragma unroll
                             for (int j = 0; j < NJ; ++j)
-                                o[(int64_t)row * p.ldo + j * 16] = Op::kScaled ? (Out)((float)__float_as_int(v[j][r]) * col_scale[Op::kScaled ? j : 0] * w4[r]) : (Out)(v[j][r] * w4[r]);
+                                o[(int64_t)row * p.ldo + j * 16] = (Out)(v[j][r] * w4[r]);
                         }
                     }
                 });
@@ -887,7 +932,7 @@ __device__ __forceinline__ void gemm_tile(const GemmParams& p, const TileCoord& 
 #pragma unroll
                         for (int j = 0; j < NJ; ++j)
                             if (!split_extra || j / (NJ / 2) == wm)      // split: this wavefront row's half
-                                o[(int64_t)row * p.ldo + j * 16] = Op::kScaled ? (Out)((float)accE[j][r] * col_scale[Op::kScaled ? j : 0] * wr) : (Out)(accE[j][r] * wr);
+                                o[(int64_t)row * p.ldo + j * 16] = Op::kScaled ? (Out)((float)bits(accE[j][r]) * col_scale[Op::kScaled ? j : 0] * wr) : (Out)(accE[j][r] * wr);
                     }
                 }
             }

@@ -213,11 +213,6 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
         if (tid < BM) row_scales[tid] = row_scale;
         if (MODE == 1) __syncthreads();
     }
-    // row `row` of the block, fragment b: the sum as a float
-    auto value = [&](int row, int b, auto sum) __attribute__((always_inline)) -> float {
-        if constexpr (Op::kScaled) return (float)sum * col_scale[b] * row_scales[row];
-        else return sum;
-    };
 
     if constexpr (MODE == 0) {
         // h leaves through LDS in whole lines, 16 bytes a lane, in part past the L2 (see kStreamRows)
@@ -230,7 +225,10 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
 #pragma unroll
                     for (int f = 0; f < FC; ++f) {
                         const int row = i * 16 + g * 4 + v;
-                        *(__bf16*)(smem + row * kOutRow + (cw * 16 * FC + f * 16 + r) * 2) = (__bf16)silu_mul_bf16(value(row, f, acc[i][f][v]), value(row, NB - FC + f, acc[i][NB - FC + f][v]));
+                        float y;
+                        if constexpr (Op::kScaled) y = silu_mul_i8(acc[i][f][v], acc[i][NB - FC + f][v], col_scale[f] * kGateFactor, col_scale[NB - FC + f] * kUpFactor, row_scales[row]);
+                        else y = silu_mul_bf16(acc[i][f][v], acc[i][NB - FC + f][v]);
+                        *(__bf16*)(smem + row * kOutRow + (cw * 16 * FC + f * 16 + r) * 2) = (__bf16)y;
                     }
         __syncthreads();
         constexpr int kChunks = kCols / 8;           // 16-byte chunks of a row
@@ -262,7 +260,7 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
                 const int64_t o = (int64_t)(row0 + row) * p.ldo + col;
                 if constexpr (Op::kScaled) {
 #pragma unroll
-                    for (int f = 0; f < FC; ++f) ((typename Op::Out*)p.out)[o + f * 16] = (typename Op::Out)value(row, f, acc[i][f][v]);
+                    for (int f = 0; f < FC; ++f) ((typename Op::Out*)p.out)[o + f * 16] = (typename Op::Out)((float)acc[i][f][v] * col_scale[f] * row_scales[row]);
                 } else {
                     const float wgt = p.row_w ? p.row_w[row0 + row] : 1.0f;
 #pragma unroll

@@ -130,11 +130,8 @@ __global__ __launch_bounds__(64 * CW) void ffn_thin(const GemmParams p) {
             const float s = __shfl(row_scale, orow, 64);
             if (orow >= rows_here) continue;
             const int64_t o = (int64_t)(row0 + orow) * p.ldo + col;
-            float y[NB];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) y[b] = (float)acc[b][v] * col_scale[b] * s;
-            if constexpr (MODE == 0) ((__bf16*)p.out)[o] = (__bf16)silu_mul_bf16(y[0], y[1]);
-            else ((typename Op::Out*)p.out)[o] = (typename Op::Out)y[0];
+            if constexpr (MODE == 0) ((__bf16*)p.out)[o] = (__bf16)silu_mul_i8(acc[0][v], acc[NB - 1][v], col_scale[0] * kGateFactor, col_scale[NB - 1] * kUpFactor, s);
+            else ((typename Op::Out*)p.out)[o] = (typename Op::Out)((float)acc[0][v] * col_scale[0] * s);
             continue;
         }
         if (orow >= rows_here) continue;

@@ -50,150 +50,238 @@ __device__ __forceinline__ uint32_t quantized(const f32x4& v, const RowScale& s)
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
 }
 
-__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ __forceinline__ f32x4 load4(const uint16_t* p) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+// FAR: with the non-temporal hint.  What is read here is read for the last time, and with the hint it comes faster where it does not come from the caches: us in a graph
+// over buffers that exceed the last-level cache, without / with, rows in 8 bits 14336 x 4096 bf16 (176 MB) 32.0 / 30.6 (5.76 TB/s), float32 9857 x 4096 36.4 / 33.8; norm
+// 9857 x 6144 (787 MB) 140 / 132 (5.96 TB/s), 30000 x 1024 84 / 77, but 4000 x 4096 (246 MB) 42.3 / 43.9.  What is written is read next: written with the hint the same
+// calls take 29.1 and 131, and who reads the 8-bit rows 25 and 30 more.  Except h between two launches that stream weights (`past`): lines that the caches have
+// to write back cost these more (experts of the Mixtral-8x7B shape, 256 tokens 260 / 248).  hidden_out, which nobody wants for a layer, takes the hint too.
+constexpr int64_t kQuantizeFar = (int64_t)16 << 20, kNormFar = (int64_t)256 << 20;      // more bytes than these
+template <bool FAR, class V>
+__device__ __forceinline__ V load_as(const void* p) {
+    return FAR ? __builtin_nontemporal_load(reinterpret_cast<const V*>(p)) : *reinterpret_cast<const V*>(p);
+}
+template <bool FAR, class V>
+__device__ __forceinline__ void store_as(void* p, V v) {
+    if constexpr (FAR) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+    else *reinterpret_cast<V*>(p) = v;
+}
+__device__ __forceinline__ f32x4 widened(uint32_t a, uint32_t b) {   // four bf16
+    return f32x4{__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u), __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
 }
 
-constexpr int kThreads = 256;
+// VEC elements of a row as they lie in memory, 8 or 16 bytes.
+template <class In, int VEC>
+struct Piece;
+template <>
+struct Piece<float, 4> {
+    typedef f32x4 Raw;
+    typedef uint32_t Out;
+    __device__ static uint32_t most(const Raw& v) { return magnitude(v); }
+    __device__ static Out quantized4(const Raw& v, const RowScale& s) { return quantized(v, s); }
+};
+template <>
+struct Piece<uint16_t, 4> {
+    typedef u32x2 Raw;
+    typedef uint32_t Out;
+    __device__ static uint32_t most(const Raw& v) { return magnitude(widened(v.x, v.y)); }
+    __device__ static Out quantized4(const Raw& v, const RowScale& s) { return quantized(widened(v.x, v.y), s); }
+};
+template <>
+struct Piece<uint16_t, 8> {
+    typedef u32x4 Raw;
+    typedef u32x2 Out;
+    __device__ static uint32_t most(const Raw& v) { return max(magnitude(widened(v.x, v.y)), magnitude(widened(v.z, v.w))); }
+    __device__ static Out quantized4(const Raw& v, const RowScale& s) { return Out{quantized(widened(v.x, v.y), s), quantized(widened(v.z, v.w), s)}; }
+};
 
-// A block to a row.  PER vectors of four elements to a thread stay in registers; with PER = 0 the row is read twice.
-template <class In, int PER>
-__global__ __launch_bounds__(kThreads) void quantize_kernel(const In* __restrict__ x, int64_t row_elements, int T, int vectors, uint32_t* __restrict__ q,
-                                                            float* __restrict__ scale) {
-    __shared__ uint32_t part[kThreads / 64];
-    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+constexpr int kMostBlocks = 1 << 20;             // rows beyond theirs are taken in turn
+
+// WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is read twice.
+template <class In, int VEC, int WAVES, int PER, bool FAR, bool PAST>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel(const In* __restrict__ x, int64_t row_elements, int T, int pieces, int8_t* __restrict__ q,
+                                                                                 float* __restrict__ scale) {
+    typedef Piece<In, VEC> P;
+    __shared__ uint32_t part[WAVES];
+    constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = 64 * WAVES;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int me = WAVES == 1 ? lane : threadIdx.x;
+    for (int64_t t = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); t < T; t += (int64_t)gridDim.x * kRows) {
         const In* const row = x + t * row_elements;
-        uint32_t* const out = q + t * vectors;
-        f32x4 v[PER ? PER : 1];
+        int8_t* const out = q + t * pieces * VEC;
+        typename P::Raw v[PER ? PER : 1];
         uint32_t most = 0;
         if constexpr (PER > 0) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int c = threadIdx.x + i * kThreads;
-                v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (c < vectors) v[i] = load4(row + 4 * c);
+                const int c = me + i * kThreads;
+                v[i] = typename P::Raw{};
+                if (c < pieces) v[i] = load_as<FAR, typename P::Raw>(row + VEC * c);
             }
 #pragma unroll
-            for (int i = 0; i < PER; ++i) most = max(most, magnitude(v[i]));
+            for (int i = 0; i < PER; ++i) most = max(most, P::most(v[i]));
         } else {
-            for (int c = threadIdx.x; c < vectors; c += kThreads) most = max(most, magnitude(load4(row + 4 * (int64_t)c)));
+            for (int c = me; c < pieces; c += kThreads) most = max(most, P::most(load_as<false, typename P::Raw>(row + (int64_t)VEC * c)));
         }
         most = wave_max(most);
-        __syncthreads();                         // the row before this one has read `part`
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-        __syncthreads();
-        const RowScale s = scale_of(max(max(part[0], part[1]), max(part[2], part[3])));
+        if constexpr (WAVES > 1) {
+            __syncthreads();                     // the row before this one has read `part`
+            if (lane == 0) part[wave] = most;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = max(most, part[w]);
+        }
+        const RowScale s = scale_of(most);
         if constexpr (PER > 0) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int c = threadIdx.x + i * kThreads;
-                if (c < vectors) out[c] = quantized(v[i], s);
+                const int c = me + i * kThreads;
+                if (c < pieces) store_as<PAST>(out + VEC * c, P::quantized4(v[i], s));
             }
         } else {
-            for (int c = threadIdx.x; c < vectors; c += kThreads) out[c] = quantized(load4(row + 4 * (int64_t)c), s);
+            for (int c = me; c < pieces; c += kThreads) store_as<false>(out + (int64_t)VEC * c, P::quantized4(load_as<false, typename P::Raw>(row + (int64_t)VEC * c), s));
         }
-        if (threadIdx.x == 0) scale[t] = s.scale;
+        if (me == 0) scale[t] = s.scale;
     }
 }
 
-constexpr int kMostBlocks = 1 << 20;             // rows beyond them are taken in turn
-
-template <class In>
-int launch_quantize(int T, int N, const In* x, int64_t row_elements, int8_t* q, float* scale, hipStream_t st) {
-    const dim3 grid(std::min(T, kMostBlocks)), block(kThreads);
-    const int vectors = N / 4, per = (vectors + kThreads - 1) / kThreads;
-    if (per <= 4) hipLaunchKernelGGL((quantize_kernel<In, 4>), grid, block, 0, st, x, row_elements, T, vectors, (uint32_t*)q, scale);
-    else if (per <= 16) hipLaunchKernelGGL((quantize_kernel<In, 16>), grid, block, 0, st, x, row_elements, T, vectors, (uint32_t*)q, scale);
-    else hipLaunchKernelGGL((quantize_kernel<In, 0>), grid, block, 0, st, x, row_elements, T, vectors, (uint32_t*)q, scale);
+template <class In, int VEC, int WAVES, int PER>
+int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, hipStream_t st) {
+    const dim3 grid(std::min(WAVES == 1 ? (T + 3) / 4 : T, kMostBlocks)), block(WAVES == 1 ? 256 : 64 * WAVES);
+    const bool far = (int64_t)T * pieces * VEC * ((int)sizeof(In) + 1) > kQuantizeFar;
+    if (past) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, true>), grid, block, 0, st, x, row_elements, T, pieces, q, scale);
+    else if (far) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale);
+    else hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, false, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }
 
-// One block per row, as add_rmsnorm_kernel (moe_dense.hip): s = hidden + delta stays in registers, its squares are added up, then the
-// magnitudes of y are compared.
-constexpr int kMaxVec = 8;                       // vectors of four to a thread: H <= 8192
+// Wavefronts by the length of the row alone: a row's loads are then under way at once, and what is in flight fills the chip.  us, 256 threads to
+// every row / these: 512 x 14336 9.1 / 5.9, 8192 x 14336 88 / 64, 60000 x 256 53 / 17, 1 x 28672 10.4 / 3.2.
+template <class In, int VEC>
+int launch_quantize(int T, int N, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, hipStream_t st) {
+    const int pieces = N / VEC;
+    if (pieces <= 64) return launch_quantize<In, VEC, 1, 1>(T, pieces, x, row_elements, q, scale, past, st);
+    if (pieces <= 128) return launch_quantize<In, VEC, 1, 2>(T, pieces, x, row_elements, q, scale, past, st);
+    if (pieces <= 512) return launch_quantize<In, VEC, 4, 2>(T, pieces, x, row_elements, q, scale, past, st);
+    if (pieces <= 1024) return launch_quantize<In, VEC, 8, 2>(T, pieces, x, row_elements, q, scale, past, st);
+    if (pieces <= 2048) return launch_quantize<In, VEC, 16, 2>(T, pieces, x, row_elements, q, scale, past, st);
+    if (pieces <= 4096) return launch_quantize<In, VEC, 16, 4>(T, pieces, x, row_elements, q, scale, past, st);
+    return launch_quantize<In, VEC, 16, 0>(T, pieces, x, row_elements, q, scale, past, st);
+}
+
+// Residual and norm: one pass over the rows.  s = hidden + delta stays in registers, its squares are added up, then the magnitudes of y are
+// compared; gamma comes while the sums are formed.  How many wavefronts a row has goes by H alone, so that a row's sum, and with it its bits, are the
+// same in every call.
+constexpr int kMostH = 8192;
 
 struct NormArgs {
     const float *hidden, *delta, *gamma;
     float* hidden_out;
     uint16_t* x_out;
-    uint32_t* q;
+    int8_t* q;
     float* scale;
     float eps;
-    int T, vectors;
+    int T, vectors;                              // of four elements
 };
 
-template <int PER>
-__global__ __launch_bounds__(kThreads) void add_rmsnorm_i8_kernel(const NormArgs a) {
-    __shared__ float sums[kThreads / 64];
-    __shared__ uint32_t part[kThreads / 64];
+template <int WAVES, int PER, bool FAR>
+__global__ __launch_bounds__(64 * WAVES) void add_rmsnorm_i8_kernel(const NormArgs a) {
+    __shared__ float sums[WAVES];
+    __shared__ uint32_t part[WAVES];
+    constexpr int kThreads = 64 * WAVES;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         const int64_t row = t * a.vectors;
-        f32x4 v[PER];
+        f32x4 v[PER], g[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int c = threadIdx.x + i * kThreads;
+            v[i] = g[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (c < a.vectors) v[i] = load_as<FAR, f32x4>(a.delta + 4 * (row + c));
+        }
+        if (a.hidden)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int c = threadIdx.x + i * kThreads;
+                if (c < a.vectors) g[i] = load_as<FAR, f32x4>(a.hidden + 4 * (row + c));
+            }
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = threadIdx.x + i * kThreads;
-            v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (a.hidden) v[i] += g[i];
             if (c < a.vectors) {
-                v[i] = load4(a.delta + 4 * (row + c));
-                if (a.hidden) v[i] += load4(a.hidden + 4 * (row + c));
+                g[i] = load_as<false, f32x4>(a.gamma + 4 * c);
+                if (a.hidden_out) store_as<FAR>(a.hidden_out + 4 * (row + c), v[i]);
             }
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int c = threadIdx.x + i * kThreads;
-            if (c < a.vectors && a.hidden_out) *reinterpret_cast<f32x4*>(a.hidden_out + 4 * (row + c)) = v[i];
             ss += (v[i].x * v[i].x + v[i].y * v[i].y) + (v[i].z * v[i].z + v[i].w * v[i].w);
         }
 #pragma unroll
         for (int m = 32; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
-        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = ss;
-        __syncthreads();
-        const float r = 1.f / sqrtf(((sums[0] + sums[1]) + (sums[2] + sums[3])) / (float)(a.vectors * 4) + a.eps);
+        if constexpr (WAVES > 1) {
+            if (lane == 0) sums[wave] = ss;
+            __syncthreads();
+            ss = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) ss += sums[w];
+        }
+        const float r = 1.f / sqrtf(ss / (float)(a.vectors * 4) + a.eps);
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int c = threadIdx.x + i * kThreads;
-            if (c < a.vectors) v[i] = v[i] * r * load4(a.gamma + 4 * c);
-            most = max(most, magnitude(v[i]));
+            v[i] = v[i] * r * g[i];
+            if (threadIdx.x + i * kThreads < a.vectors) most = max(most, magnitude(v[i]));      // what is behind the row is 0 * r, which may be NaN
         }
         most = wave_max(most);
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-        __syncthreads();                         // also: everyone has read `sums`
-        const RowScale s = scale_of(max(max(part[0], part[1]), max(part[2], part[3])));
+        if constexpr (WAVES > 1) {
+            if (lane == 0) part[wave] = most;
+            __syncthreads();                     // also: everyone has read `sums`
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = max(most, part[w]);
+        }
+        const RowScale s = scale_of(most);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = threadIdx.x + i * kThreads;
             if (c >= a.vectors) continue;
-            if (a.x_out) *reinterpret_cast<u32x2*>(a.x_out + 4 * (row + c)) = __builtin_bit_cast(u32x2, __builtin_convertvector(v[i], bf16x4));      // to nearest even
-            a.q[row + c] = quantized(v[i], s);
+            if (a.x_out) store_as<false>(a.x_out + 4 * (row + c), __builtin_bit_cast(u32x2, __builtin_convertvector(v[i], bf16x4)));      // to nearest even
+            store_as<false>(a.q + 4 * (row + c), quantized(v[i], s));
         }
         if (threadIdx.x == 0) a.scale[t] = s.scale;
     }
+}
+
+template <int WAVES, int PER>
+int launch_norm(const NormArgs& a, hipStream_t st) {
+    const dim3 grid(std::min(a.T, kMostBlocks)), block(64 * WAVES);
+    if ((int64_t)a.T * a.vectors * 4 * 13 > kNormFar) hipLaunchKernelGGL((add_rmsnorm_i8_kernel<WAVES, PER, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((add_rmsnorm_i8_kernel<WAVES, PER, false>), grid, block, 0, st, a);
+    MOE_HIP_TRY(hipGetLastError());
+    return MOE_OK;
 }
 
 }  // namespace
 
 namespace moe {
 
-int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, hipStream_t st) {
-    return x_dtype == MOE_DTYPE_F32 ? launch_quantize(T, N, (const float*)x, row_elements, q, scale, st) : launch_quantize(T, N, (const uint16_t*)x, row_elements, q, scale, st);
+int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, hipStream_t st) {
+    if (x_dtype == MOE_DTYPE_F32) return launch_quantize<float, 4>(T, N, (const float*)x, row_elements, q, scale, past, st);
+    if (N % 8 == 0 && row_elements % 8 == 0 && aligned16(x) && (uintptr_t)q % 8 == 0) return launch_quantize<uint16_t, 8>(T, N, (const uint16_t*)x, row_elements, q, scale, past, st);
+    return launch_quantize<uint16_t, 4>(T, N, (const uint16_t*)x, row_elements, q, scale, past, st);
 }
 
 int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* q, float* scale,
                           hipStream_t st) {
-    const NormArgs a{hidden, delta, gamma, hidden_out, (uint16_t*)x_out, (uint32_t*)q, scale, eps, T, H / 4};
-    const dim3 grid(std::min(T, kMostBlocks)), block(kThreads);
-    if (a.vectors <= 4 * kThreads) hipLaunchKernelGGL((add_rmsnorm_i8_kernel<4>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((add_rmsnorm_i8_kernel<kMaxVec>), grid, block, 0, st, a);
-    MOE_HIP_TRY(hipGetLastError());
-    return MOE_OK;
+    const NormArgs a{hidden, delta, gamma, hidden_out, (uint16_t*)x_out, q, scale, eps, T, H / 4};
+    if (H <= 256) return launch_norm<1, 1>(a, st);
+    if (H <= 1024) return launch_norm<4, 1>(a, st);
+    if (H <= 2048) return launch_norm<4, 2>(a, st);
+    if (H <= 4096) return launch_norm<8, 2>(a, st);
+    if (H <= 6144) return launch_norm<8, 3>(a, st);
+    return launch_norm<8, 4>(a, st);
 }
 
-bool norm_takes(int32_t H, float eps) { return H > 0 && H % 4 == 0 && H <= 4 * kThreads * kMaxVec && eps >= 0.f; }
+bool norm_takes(int32_t H, float eps) { return H > 0 && H % 4 == 0 && H <= kMostH && eps >= 0.f; }
 
 }  // namespace moe
 
@@ -206,7 +294,7 @@ int moe_quantize_i8(int32_t T, int32_t N, const void* x, int32_t x_dtype, int64_
     const int64_t esize = x_dtype == MOE_DTYPE_F32 ? 4 : 2, x_bytes = ((T - 1) * row_elements + N) * esize, q_bytes = (int64_t)T * N, s_bytes = (int64_t)T * 4;
     if (!x || !x_q || !x_scale || (uintptr_t)x % (4 * esize) != 0 || (uintptr_t)x_q % 4 != 0 || (uintptr_t)x_scale % 4 != 0) return MOE_ERR_INVALID_ARG;
     if (overlap(x, x_bytes, x_q, q_bytes) || overlap(x, x_bytes, x_scale, s_bytes) || overlap(x_q, q_bytes, x_scale, s_bytes)) return MOE_ERR_INVALID_ARG;
-    return launch_quantize_i8(T, N, x, x_dtype, row_elements, x_q, x_scale, (hipStream_t)stream);
+    return launch_quantize_i8(T, N, x, x_dtype, row_elements, x_q, x_scale, false, (hipStream_t)stream);
 }
 
 int moe_add_rmsnorm_i8(int32_t T, int32_t H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* x_q,
