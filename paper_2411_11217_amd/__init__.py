@@ -17,4 +17,4 @@ from .binding import (  # noqa: F401
     AttnWorkspace, KvShape, KvStep, attn_workspace_bytes, kv_validate, make_kv_shape, moe_attn_decode, moe_kv_assign, moe_qk_norm_rope,
 )
 from .paged import PagedWeights  # noqa: F401
-from .decode import DecodeLayers, LayerWeights  # noqa: F401
+from .decode import DecodeLayers, LayerScales, LayerWeights  # noqa: F401

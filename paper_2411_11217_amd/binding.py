@@ -737,9 +737,9 @@ def moe_add_rmsnorm_i8(hidden, delta, gamma, eps: float, want_hidden: bool = Tru
     pg = _dev(gamma, torch.float32, (H,), "gamma")
     dev = delta.device
     with _on(stream):
-        hs = torch.empty((T, H), dtype=torch.float32, device=dev) if want_hidden else None
-        x = torch.empty((T, H), dtype=torch.bfloat16, device=dev) if want_x else None
-        x_q = torch.empty((T, H), dtype=torch.int8, device=dev)
+        hs = torch.empty_like(delta) if want_hidden else None                  # half as long as torch.empty
+        x = torch.empty_like(delta, dtype=torch.bfloat16) if want_x else None
+        x_q = torch.empty_like(delta, dtype=torch.int8)
         x_scale = torch.empty(T, dtype=torch.float32, device=dev)
     _check(_lib().moe_add_rmsnorm_i8(T, H, ph, pd, pg, float(eps), None if hs is None else hs.data_ptr(), None if x is None else x.data_ptr(), x_q.data_ptr(),
                                      x_scale.data_ptr(), _stream(stream)), "moe_add_rmsnorm_i8")
@@ -774,8 +774,8 @@ def moe_expert_ffn_i8(s: MoEShape, x_q, x_scale, offsets, page_table, page_pool,
     pw = _optional(row_w, torch.float32, (R,), "row_w")
     ps = _optional(status, torch.int32, (4,), "status")
     with _on(stream):
-        h = torch.empty((R, s.F), dtype=torch.bfloat16, device=x_q.device)
         h_q = torch.empty((R, s.F), dtype=torch.int8, device=x_q.device)
+        h = torch.empty_like(h_q, dtype=torch.bfloat16)
         h_scale = torch.empty(R, dtype=torch.float32, device=x_q.device)
         out = torch.empty((R, s.H), dtype=torch.bfloat16, device=x_q.device)
     _check(_lib().moe_expert_ffn_i8(ctypes.byref(s), px, pxs, pr, po, pt, pp, int(page_pool.shape[0]), scales.pointers(s), pw, h.data_ptr(), h_q.data_ptr(),

@@ -6,6 +6,9 @@ batch of requests -- whole prompts, single tokens, or both in one step -- with t
                      (moe_qk_norm_rope), attention over the cache (moe_attn_decode), O projection + residual + norm + MoE layer
                      (moe_post_attention)
 
+With a shape of 8-bit integers the projections and the experts are products of those (moe_pre_attention_i8, moe_post_attention_i8), and every layer
+brings the scales of its weights' output channels.
+
 In the paper's decode stage the attention of the middle line runs on the CPU (its section 4.1); here all of a layer is on the GPU.  The
 order of the calls and the buffers between them, nothing else: all arithmetic is the library's.
 """
@@ -17,6 +20,14 @@ from typing import List, Optional, Sequence, Tuple
 import torch
 
 from . import binding as B
+
+
+@dataclasses.dataclass
+class LayerScales:
+    """Scales of one layer's 8-bit weights, device float32: of the rows of Wqkv and Wo, and of the experts'."""
+    qkv: torch.Tensor                    # [rows of Wqkv, padded to a multiple of 128]
+    o: torch.Tensor                      # [H]
+    experts: B.ExpertScales
 
 
 @dataclasses.dataclass
@@ -32,6 +43,7 @@ class LayerWeights:
     bias: Optional[torch.Tensor] = None
     q_gamma: Optional[torch.Tensor] = None
     k_gamma: Optional[torch.Tensor] = None
+    scales: Optional[LayerScales] = None         # with 8-bit weights
 
 
 class DecodeLayers:
@@ -40,8 +52,11 @@ class DecodeLayers:
 
     def __init__(self, shape: B.MoEShape, kv: B.KvShape, layers: Sequence[LayerWeights], inv_freq: torch.Tensor, n_requests: int,
                  eps: float = 1e-5, window: int = 0, device="cuda"):
-        if kv.dtype != B.DTYPE_BF16 or shape.dtype != B.DTYPE_BF16:
-            raise ValueError("DecodeLayers: cache and MoE layer have to be bf16, the type of the projections beside them")
+        if kv.dtype != B.DTYPE_BF16 or shape.dtype not in (B.DTYPE_BF16, B.DTYPE_I8):
+            raise ValueError("DecodeLayers: cache and MoE layer have to be bf16, the type of the projections beside them (or layer and projections 8-bit integers)")
+        for i, w in enumerate(layers):
+            if (w.scales is not None) != (shape.dtype == B.DTYPE_I8):
+                raise ValueError(f"DecodeLayers: layer {i}: scales go with 8-bit weights, and with no others")
         if not 0 <= n_requests <= B.MAX_REQUESTS:
             raise ValueError(f"n_requests: at most {B.MAX_REQUESTS}, got {n_requests}")
         self.shape, self.kv, self.layers, self.n_requests = shape, kv, list(layers), int(n_requests)
@@ -51,7 +66,7 @@ class DecodeLayers:
         for status in (B.kv_validate(kv), B.validate_shape(shape)):
             B._check(status, "DecodeLayers")
         for K, N in ((shape.H, self.qkv_width), (self.attn_width, shape.H)):
-            B.linear_pages_required(B.make_linear_shape(1, K, N, shape.page_bytes))         # raises where the projections do not take such sizes
+            B.linear_pages_required(B.make_linear_shape(1, K, N, shape.page_bytes, shape.dtype))         # raises where the projections do not take such sizes
         self.caches: List[Tuple[torch.Tensor, torch.Tensor]] = [
             (torch.empty(kv.cache_shape, dtype=kv.torch_dtype, device=device), torch.empty(kv.cache_shape, dtype=kv.torch_dtype, device=device)) for _ in self.layers]
         self.block_table = torch.full((self.n_requests, kv.max_pages), -1, dtype=torch.int32, device=device)
@@ -76,16 +91,23 @@ class DecodeLayers:
         B.moe_kv_assign(kv, self.lengths, fresh, self.free_pages, self.free_head, self.block_table, step=tables, status=self.status)
         seen = torch.where(tables.slots >= 0, tables.positions + 1, 0)          # rows without a slot attend to nothing
         s = self.shape.with_tokens(T)
-        qkv_proj = B.make_linear_shape(T, s.H, self.qkv_width, s.page_bytes)
-        o_proj = B.make_linear_shape(T, self.attn_width, s.H, s.page_bytes)
+        qkv_proj = B.make_linear_shape(T, s.H, self.qkv_width, s.page_bytes, s.dtype)
+        o_proj = B.make_linear_shape(T, self.attn_width, s.H, s.page_bytes, s.dtype)
         hidden, delta = None, embedded
         for w, (k_cache, v_cache) in zip(self.layers, self.caches):
-            hidden, _, qkv, _ = B.moe_pre_attention(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, want_bf16=False)
+            if w.scales is None:
+                hidden, _, qkv, _ = B.moe_pre_attention(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, want_bf16=False)
+            else:
+                hidden, _, _, qkv = B.moe_pre_attention_i8(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, w.scales.qkv, status=self.status)
             q = B.moe_qk_norm_rope(kv, qkv, self.inv_freq, tables.positions, tables.slots, k_cache, v_cache, w.q_gamma, w.k_gamma, self.eps, status=self.status)
             attn, _ = B.moe_attn_decode(kv, q, seen, self.block_table, k_cache, v_cache, window=self.window, table_row=tables.request,
                                         workspace=self._workspace, status=self.status)
-            hidden, _, delta, _ = B.moe_post_attention(s, o_proj, attn.view(T, self.attn_width), hidden, w.o_table, w.norm_moe, self.eps, w.Wr,
-                                                       w.page_table, w.page_pool, bias=w.bias)
+            attn = attn.view(T, self.attn_width)
+            if w.scales is None:
+                hidden, _, delta, _ = B.moe_post_attention(s, o_proj, attn, hidden, w.o_table, w.norm_moe, self.eps, w.Wr, w.page_table, w.page_pool, bias=w.bias)
+            else:
+                hidden, _, delta, _ = B.moe_post_attention_i8(s, o_proj, attn, hidden, w.o_table, w.scales.o, w.norm_moe, self.eps, w.Wr, w.page_table, w.page_pool,
+                                                              w.scales.experts, bias=w.bias)
         out = hidden + delta
         self.lengths, self.free_head, self._turn = tables.seq_len, tables.free_head, self._turn ^ 1
         return out, tables

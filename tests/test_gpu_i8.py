@@ -354,6 +354,22 @@ def test_experts_rows_are_their_own(T):
         assert torch.equal(a.cpu()[of_bad], b.cpu()[of_bad])
 
 
+def test_experts_rows_have_the_same_bits_in_every_kernel():
+    """1, 30, 75 and up to 1000 rows per expert on average are the kernels for a handful of tokens, for few rows (two blocks), and blocks of 256 rows (halved, narrow)."""
+    x = Experts(512, 1024, 2, 1, 65536)
+    q, scale = x.rows(2000)
+    ids = torch.randint(0, 2, (2000, 1), generator=x.g)
+    ids[:3] = torch.tensor([[0], [1], [0]])
+    first = None
+    for T in (3, 60, 150, 300, 900, 2000):
+        offsets, row_src, _ = x.routing(T, ids[:T])
+        got = x.run(T, q[:T], scale[:T], offsets, row_src, None)
+        at = [int((row_src == t).nonzero()) for t in range(3)]
+        mine = [t.cpu()[at] for t in got]
+        first = first or mine
+        assert all(torch.equal(a, b) for a, b in zip(first, mine)), T
+
+
 @pytest.mark.parametrize("T", [4, 100, 900])
 def test_experts_bad_pages(T):
     x = Experts(256, 512, 4, 2, 16384)
