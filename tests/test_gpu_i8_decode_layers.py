@@ -65,7 +65,7 @@ def test_a_step_is_its_calls():
             delta = M.moe_combine(st, o, p["row_of"])
         assert torch.equal(out, hidden + delta)
         assert model.status.tolist() == [0] * 4 and status[0] == 0
-    assert model.lengths.tolist() == [9, 7, 35]
+    assert model.lengths.tolist() == [7 + 1 + 1, 5 + 1, 3 + 1 + 1 + 30]
 
 
 def test_prompts_at_once_and_token_by_token():
