@@ -19,6 +19,15 @@ typedef Int8<__bf16> ToBf16;
 constexpr int kUnits = 256;                  // compute units
 constexpr int kTileRows = 256;               // of the blocks of moe_ffn_gemm.h
 
+// The kernel for few rows up to this many rows per expert on average.  us for the call, that kernel / the 256-row blocks: Mixtral-8x7B shape 37 rows 242 / 250, 75: 256 / 263, 100: 268 / 273, 125: 356 /
+// 286; 2048 x 4096 64: 59.3 / 61.2, 100: 63.7 / 63.8, 125: 79 / 66; 1024 x 2816 80: 38.1 / 38.5, 100: 40.5 / 39.2; 64 experts of 2048 x 1024 80: 96 / 107, 100: 102 / 111, 125: 128 / 117; DBRX shape 80: 557 / 571,
+// 100: 580 / 580; 40 % of the rows on one expert, 2048 x 4096 64: 67.5 / 74, 100: 73 / 75, Mixtral-8x7B shape 64: 282 / 296, 100: 322 / 327.
+constexpr int kFewRows = 96;
+// Weights with the non-temporal hint beyond this many bytes: half of the last-level cache.  A layer's weights are still there from the call before only in a program that has no other layer.  us,
+// without / with the hint, 2048 x 4096 (201 MB), the same weights in every call | three layers in turn: 16 tokens 40 / 38 | 45 / 41, 100: 46 / 51 | 53 / 50, 400: 57 / 63 | 63 / 61; 1024 x 2816 (69 MB) 100
+// tokens 28 / 30 | 28 / 31, six layers 32 / 31.  Mixtral-8x7B shape 64 tokens 255 / 231, 256: 288 / 252, 1000: 421 / 389.
+constexpr int64_t kHintBytes = (int64_t)128 << 20;
+
 int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st) {
     const int R = s.T * s.k, rows_each = R / s.E;
     const Geom g = geometry(s);
@@ -40,9 +49,9 @@ int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st)
     p.w_scale = a.scales.w1;
     p.w_scale_up = a.scales.w3;
     // as launch_expert_ffn_bf16 (moe_ffn_bf16.hip)
-    const bool streams = rows_each <= 256 && (int64_t)s.E * 3 * s.H * s.F > ((int64_t)256 << 20);
+    const bool streams = rows_each <= 256 && (int64_t)s.E * 3 * s.H * s.F > kHintBytes;
     p.stream = !streams ? 0 : s.F >= 6144 && s.E * g.dt >= kUnits ? 2 : 1;
-    const bool few = rows_kernel_takes(rows_each);
+    const bool few = rows_each <= kFewRows;
     const int64_t row_tiles_each = std::max<int64_t>(1, (rows_each - p.tall_rows + kTileRows - 1) / kTileRows);
     auto half_round = [&]() {
         const int64_t last = s.E * row_tiles_each * p.NT % kUnits;
@@ -96,7 +105,15 @@ int launch_linear_i8(const LinearI8Args& a, hipStream_t st) {
     p.balance = get_opt(OPT_BALANCE);
     p.chunked = std::min(std::max(get_opt(OPT_CHUNKED), 0), 32);
     // as launch_linear_bf16 (moe_ffn_bf16.hip)
-    if (linear_takes_rows_kernel(a.T, a.K / 2, a.N)) return linear_rows<ToFloat>(p, a.N, a.T, st);
+    if (linear_takes_rows_kernel(a.T, a.K / 2, a.N)) {
+        // Teams that share k, since sums of whole numbers are exact in any order: a block's way through all of k is what a launch of one round waits for.  us, one team /
+        // four (of eight wavefronts: two) / for up to 32 rows and one group of columns eight, weights where the call before left them | from HBM: 4096 x 6144 1 row 11.1 / 9.6 /
+        // 9.4 | 13.7 / 10.3 / 10.2, 40: 13.5 / 11.9 | 16.4 / 13.3, 256: 19.2 / 18.5 | 21.4 / 19.9; 4096 x 4096 1: 10.2 / 8.5 / 7.9 | 12.3 / 8.3 / 8.3, 256: 16.7 / 15.0 | 18.3 / 15.7; 14336 x 4096 1: 30.6 / 18.0 / 17.2 |
+        // 35.3 / 20.0 / 19.5, 100: 40.8 / 30.3 | 44.8 / 32.3; 2048 x 4096 40: 9.0 / 8.4 | 9.4 / 8.3, 256: 10.6 / 10.7 | 11.5 / 11.4.  Below 2048 the start of the teams costs what they save (1024 x 1024 64 rows
+        // 5.5 / two teams 6.4).
+        if (p.KT < 16) return linear_rows<ToFloat, 1>(p, a.N, a.T, st);
+        return p.KT < 28 ? linear_rows<ToFloat, 4>(p, a.N, a.T, st) : linear_rows<ToFloat, 8>(p, a.N, a.T, st);
+    }
     const int wide_tiles = (p.n_page_tiles + 1) / 2;
     if ((int64_t)(a.T / kTileRows + 1) * wide_tiles >= 2 * kUnits) {
         p.NT = wide_tiles;

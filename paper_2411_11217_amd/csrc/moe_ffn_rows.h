@@ -31,19 +31,24 @@ struct Num {
 };
 
 // FC: fragments of 16 columns per wavefront (MODE 0: of 16 features, gate and up)
-template <class Op, int MODE, int RT, int CW, int FC, int RG, int D>
-__global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
+// KG (the linear map of integers; for the experts' down launch two teams won nothing): KG teams of CW * RG wavefronts, each with a part of k; their whole numbers are added up at the end, which is exact in any order.
+template <class Op, int MODE, int RT, int CW, int FC, int RG, int D, int KG = 1>
+__global__ __launch_bounds__(64 * CW * RG * KG) void ffn_rows(const GemmParams p) {
     constexpr int BM = 16 * RT, NB = MODE == 0 ? 2 * FC : FC, kCols = 16 * CW * FC;
     constexpr int kPass = 8 * CW * RG;               // rows that one load instruction per thread fetches
     constexpr int AJ = (BM + kPass - 1) / kPass, kStage = AJ * kPass * 128;
     static_assert(RT % 2 == 0 && RT <= 8 && (128 % kCols == 0 || (MODE == 1 && FC == 1)) && (kPass <= BM || RG == 1 || kPass >= 16 * RG), "");
     constexpr int kOutRow = kCols * 2 + 16;          // MODE 0: bytes of a row of h in LDS, 16 of padding
-    constexpr int kSmem = MODE == 0 && BM * kOutRow > 2 * kStage ? BM * kOutRow : 2 * kStage;
+    constexpr int kTeam = CW * RG, kPartial = kTeam * ((RT + RG - 1) / RG) * NB * 1024;      // wavefronts of a team, bytes of its sums
+    constexpr int kSmem = MODE == 0 && BM * kOutRow > 2 * kStage ? BM * kOutRow : KG * 2 * kStage;
     static_assert(MODE == 1 || RG == 1, "the row groups are the linear map's");
+    static_assert(KG == 1 || (MODE == 1 && Op::kScaled && (KG - 1) * kPartial <= kSmem), "teams add up whole numbers");
     __shared__ __attribute__((aligned(1024))) char smem[kSmem];
     __shared__ float row_scales[Op::kScaled ? BM : 1];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63;
+    const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kg = KG == 1 ? 0 : wave_all / kTeam, wave = KG == 1 ? wave_all : wave_all % kTeam;
+    const int tid = KG == 1 ? threadIdx.x : wave * 64 + lane;        // in the team
     const int cw = RG == 1 ? wave : wave % CW, rg = RG == 1 ? 0 : wave / CW;
     const int r = lane & 15, g = lane >> 4;
 
@@ -67,7 +72,9 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
         const int src = p.a_gather ? min(max(p.a_gather[row0 + row] / p.a_div, 0), p.a_rows - 1) : row;
         a_off[j] = (uint32_t)src * (uint32_t)p.lda_bytes + (tid & 7) * 16;
     }
-    const char* a_base = p.a_gather ? p.A : p.A + (int64_t)row0 * p.lda_bytes;
+    // the team's k-steps; every team takes as many turns of the loop as the longest
+    const int k0 = KG == 1 ? 0 : p.KT * kg / KG, KT = KG == 1 ? p.KT : p.KT * (kg + 1) / KG - k0, turns = KG == 1 ? p.KT : (p.KT + KG - 1) / KG;
+    const char* a_base = (p.a_gather ? p.A : p.A + (int64_t)row0 * p.lda_bytes) + (KG == 1 ? 0 : k0 * 128);
     const int a_wr0 = (tid >> 3) * 128 + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
     auto a_wr = [&](int j) __attribute__((always_inline)) { return (kPass % 16 ? a_wr0 ^ ((j & 1) << 6) : a_wr0) + j * kPass * 128; };     // kPass / 2 is 4 modulo 8 or 0
     const int a_rd[2] = {r * 128 + ((g ^ ((r >> 1) & 7)) << 4), r * 128 + (((4 + g) ^ ((r >> 1) & 7)) << 4)};
@@ -88,7 +95,7 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
     constexpr int kColTiles = kOwn ? 1 : 128 / kCols;     // blocks per page tile along the columns
     const int group = kOwn ? min(nt * CW + cw, p.n_cols / 16 - 1) : 0;       // the last block may have wavefronts too many
     {
-        const int t0 = kOwn ? (group >> 3) * p.KT : (nt / kColTiles) * (MODE == 0 ? 2 : 1) * p.KT;
+        const int t0 = (kOwn ? (group >> 3) * p.KT : (nt / kColTiles) * (MODE == 0 ? 2 : 1) * p.KT) + k0;
         page = t0 / p.tpp;
         within = t0 - page * p.tpp;
         tile[0] = page_addr(page) + (int64_t)within * kTileBytes;
@@ -150,7 +157,7 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
         i32x4 areg[D][NA], breg[D][2][NB];
         int kt_load = 0;                             // k-step that the next load_b fetches
         auto load_a = [&](int s, int slot) __attribute__((always_inline)) {
-            const char* base = a_base + (int64_t)min(s, p.KT - 1) * 128;
+            const char* base = a_base + (int64_t)(KG == 1 ? min(s, KT - 1) : max(min(s, KT - 1), 0)) * 128;      // a team may have no step of its own
 #pragma unroll
             for (int j = 0; j < NA; ++j) areg[slot][j] = *(const i32x4*)(base + a_off[j]);
         };
@@ -163,11 +170,11 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
                     if constexpr (STREAM) breg[slot][hp][b] = __builtin_nontemporal_load(src);
                     else breg[slot][hp][b] = *src;
                 }
-            if (++kt_load < p.KT) advance();
+            if (++kt_load < KT) advance();
         };
         int buf = 0;
         auto step = [&](int s, int slot, bool more) __attribute__((always_inline)) {     // slot: known at compile time
-            char* st = smem + buf;
+            char* st = smem + (KG == 1 ? 0 : kg * 2 * kStage) + buf;
 #pragma unroll
             for (int j = 0; j < NA; ++j) *(i32x4*)(st + a_wr(j)) = areg[slot][j];
             __syncthreads();
@@ -183,7 +190,7 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
-                        acc[i][b] = Op::mfma(a[hp][i], breg[slot][hp][b], acc[i][b]);
+                        if (KG == 1 || s < KT) acc[i][b] = Op::mfma(a[hp][i], breg[slot][hp][b], acc[i][b]);
             if (more) load_b(slot);
             buf ^= kStage;
         };
@@ -193,12 +200,12 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
             load_b(u);
         }
         int s = 0;
-        for (; s + 2 * D <= p.KT; s += D)
+        for (; s + 2 * D <= turns; s += D)
 #pragma unroll
             for (int u = 0; u < D; ++u) step(s + u, u, true);
 #pragma unroll
         for (int u = 0; u < 2 * D - 1; ++u)
-            if (s + u < p.KT) step(s + u, u % D, s + u + D < p.KT);
+            if (s + u < turns) step(s + u, u % D, s + u + D < turns);
     };
     auto run = [&](auto stream_c) __attribute__((always_inline)) {
         if (RT > 6 && rows_here > 96) main_loop(stream_c, Num<RT>{});
@@ -210,8 +217,26 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
     else run(Num<0>{});
 
     if constexpr (Op::kScaled) {
-        if (tid < BM) row_scales[tid] = row_scale;
+        if (KG > 1) __syncthreads();                 // everyone has read the last stages
+        if (kg == 0 && tid < BM) row_scales[tid] = row_scale;
+        if constexpr (KG > 1) {
+            i32x4* const part = (i32x4*)(smem + (kg - 1) * kPartial) + wave * TPW * NB * 64 + lane;
+            if (kg > 0)
+#pragma unroll
+                for (int i = 0; i < TPW; ++i)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) part[(i * NB + b) * 64] = acc[i][b];
+        }
         if (MODE == 1) __syncthreads();
+        if constexpr (KG > 1) {
+            if (kg == 0)
+#pragma unroll
+                for (int o = 0; o < KG - 1; ++o)
+#pragma unroll
+                    for (int i = 0; i < TPW; ++i)
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) acc[i][b] += ((const i32x4*)(smem + o * kPartial))[(wave * TPW * NB + i * NB + b) * 64 + lane];
+        }
     }
 
     if constexpr (MODE == 0) {
@@ -256,7 +281,7 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int row = (tile0 + i) * 16 + g * 4 + v;
-                if (row >= rows_here || !mine || (RG > 1 && i >= tiles_mine)) continue;
+                if (row >= rows_here || !mine || (RG > 1 && i >= tiles_mine) || (KG > 1 && kg > 0)) continue;
                 const int64_t o = (int64_t)(row0 + row) * p.ldo + col;
                 if constexpr (Op::kScaled) {
 #pragma unroll
@@ -279,10 +304,10 @@ __global__ __launch_bounds__(64 * CW * RG) void ffn_rows(const GemmParams p) {
     if (bad && lane == 0 && p.status) atomicOr(p.status, 1);
 }
 
-template <class Op, int MODE, int RT, int CW, int FC, int RG, int D>
+template <class Op, int MODE, int RT, int CW, int FC, int RG, int D, int KG = 1>
 int launch_rows(GemmParams& p, int cols, int R, int n_exp, hipStream_t st) {
     p.NT = (cols / 16 + CW * FC - 1) / (CW * FC);
-    hipLaunchKernelGGL((ffn_rows<Op, MODE, RT, CW, FC, RG, D>), dim3(rows_grid(p.NT, R, 16 * RT, n_exp)), dim3(64 * CW * RG), 0, st, p);
+    hipLaunchKernelGGL((ffn_rows<Op, MODE, RT, CW, FC, RG, D, KG>), dim3(rows_grid(p.NT, R, 16 * RT, n_exp)), dim3(64 * CW * RG * KG), 0, st, p);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }
@@ -329,18 +354,20 @@ int down_rows(GemmParams& p, int H, int R, int rows_each, int n_exp, hipStream_t
 // 59 | 58 / 60 (with the blocks before).
 // Groups of wavefronts that split k change the order of the sums, which the O projection hands on to a rounding and the router: left out.  So are
 // two k-steps behind one barrier: within 5 % either way, the barriers are not what the launch waits for.
-template <class Op>
+template <class Op, int KG>
 int linear_rows(GemmParams& p, int N, int T, hipStream_t st) {
     const LinearBlock b = linear_rows_block(T, p.KT * kTileK, N);        // k as bf16 would have it in these bytes
-    if (b.rows == 128) return launch_rows<Op, 1, 8, 4, 1, 2, 4>(p, N, T, 1, st);
-    if (b.rows == 32) return b.groups == 1 ? launch_rows<Op, 1, 2, 1, 1, 2, 8>(p, N, T, 1, st) : launch_rows<Op, 1, 2, 2, 1, 2, 8>(p, N, T, 1, st);
+    // sixteen wavefronts are the most, with at most 128 registers each
+    constexpr int K8 = KG < 2 ? KG : 2, K4 = KG < 4 ? KG : 4, D = K4 == 4 ? 4 : 8;
+    if (b.rows == 128) return launch_rows<Op, 1, 8, 4, 1, 2, 4, K8>(p, N, T, 1, st);
+    if (b.rows == 32) return b.groups == 1 ? launch_rows<Op, 1, 2, 1, 1, 2, KG == 8 ? 4 : 8, KG>(p, N, T, 1, st) : launch_rows<Op, 1, 2, 2, 1, 2, D, K4>(p, N, T, 1, st);
     switch (b.groups) {
-        case 1: return launch_rows<Op, 1, 4, 1, 1, 4, 8>(p, N, T, 1, st);
-        case 2: return launch_rows<Op, 1, 4, 2, 1, 2, 6>(p, N, T, 1, st);
-        case 4: return launch_rows<Op, 1, 4, 4, 1, 1, 4>(p, N, T, 1, st);
-        case 5: return launch_rows<Op, 1, 4, 5, 1, 1, 4>(p, N, T, 1, st);
-        case 6: return launch_rows<Op, 1, 4, 6, 1, 1, 4>(p, N, T, 1, st);
-        default: return launch_rows<Op, 1, 4, 8, 1, 1, 4>(p, N, T, 1, st);
+        case 1: return launch_rows<Op, 1, 4, 1, 1, 4, D, K4>(p, N, T, 1, st);
+        case 2: return launch_rows<Op, 1, 4, 2, 1, 2, K4 == 4 ? 4 : 6, K4>(p, N, T, 1, st);
+        case 4: return launch_rows<Op, 1, 4, 4, 1, 1, 4, K4>(p, N, T, 1, st);
+        case 5: return launch_rows<Op, 1, 4, 5, 1, 1, 4, K8>(p, N, T, 1, st);
+        case 6: return launch_rows<Op, 1, 4, 6, 1, 1, 4, K8>(p, N, T, 1, st);
+        default: return launch_rows<Op, 1, 4, 8, 1, 1, 4, K8>(p, N, T, 1, st);
     }
 }
 
