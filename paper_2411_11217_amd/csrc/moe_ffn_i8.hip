@@ -107,12 +107,15 @@ int launch_linear_i8(const LinearI8Args& a, hipStream_t st) {
     // as launch_linear_bf16 (moe_ffn_bf16.hip)
     if (linear_takes_rows_kernel(a.T, a.K / 2, a.N)) {
         // Teams that share k, since sums of whole numbers are exact in any order: a block's way through all of k is what a launch of one round waits for.  us, one team /
-        // four (of eight wavefronts: two) / for up to 32 rows and one group of columns eight, weights where the call before left them | from HBM: 4096 x 6144 1 row 11.1 / 9.6 /
-        // 9.4 | 13.7 / 10.3 / 10.2, 40: 13.5 / 11.9 | 16.4 / 13.3, 256: 19.2 / 18.5 | 21.4 / 19.9; 4096 x 4096 1: 10.2 / 8.5 / 7.9 | 12.3 / 8.3 / 8.3, 256: 16.7 / 15.0 | 18.3 / 15.7; 14336 x 4096 1: 30.6 / 18.0 / 17.2 |
-        // 35.3 / 20.0 / 19.5, 100: 40.8 / 30.3 | 44.8 / 32.3; 2048 x 4096 40: 9.0 / 8.4 | 9.4 / 8.3, 256: 10.6 / 10.7 | 11.5 / 11.4.  Below 2048 the start of the teams costs what they save (1024 x 1024 64 rows
-        // 5.5 / two teams 6.4).
-        if (p.KT < 16) return linear_rows<ToFloat, 1>(p, a.N, a.T, st);
-        return p.KT < 28 ? linear_rows<ToFloat, 4>(p, a.N, a.T, st) : linear_rows<ToFloat, 8>(p, a.N, a.T, st);
+        // four (of eight wavefronts: two), weights where the call before left them | from HBM: 4096 x 6144 40 rows 13.5 / 11.9 | 16.4 / 13.3, 256: 19.2 / 18.5 | 21.4 / 19.9; 14336 x 4096 100: 40.8 / 30.3 |
+        // 44.8 / 32.3; 2048 x 4096 40: 9.0 / 8.4 | 9.4 / 8.3, 256: 10.6 / 10.7 | 11.5 / 11.4; below 2048 the start of the teams costs what they save.
+        //   Where blocks of 32 rows and 16 columns make one round: eight teams of two wavefronts, with a k of middle length, or where only 32 columns make one round, four teams of
+        // four.  us, the blocks above / 32 x 16 / 32 x 32: 4096 x 1024 100 rows 9.9 / 7.3 / 8.7, 4096 x 128 1000: 11.0 / 8.0 / 8.8, 2000: 11.9 / 16.6 / 9.9, 14336 x 512 256: 26.9 / 17.7 / 22.6, 14336 x 4096 1: 30.6 / 17.2 / 18.0,
+        // 2816 x 1024 100: 8.8 / 7.4 / 7.7, 2048 x 1024 100: 7.2 / 6.8 / 6.4, 1536 x 1024: 6.8 / 6.7 / 6.3, 1024 x 1024: 5.7 / 6.5 / 6.0.
+        const int64_t row_tiles = ((int64_t)a.T + 31) / 32;
+        if (p.KT >= 20 && row_tiles * (a.N / 16) <= kUnits) return launch_rows<ToFloat, 1, 2, 1, 1, 2, 4, 8>(p, a.N, a.T, 1, st);
+        if (p.KT >= 12 && row_tiles * (a.N / 32) <= kUnits) return launch_rows<ToFloat, 1, 2, 2, 1, 2, 4, 4>(p, a.N, a.T, 1, st);
+        return p.KT < 16 ? linear_rows<ToFloat, 1>(p, a.N, a.T, st) : linear_rows<ToFloat, 4>(p, a.N, a.T, st);
     }
     const int wide_tiles = (p.n_page_tiles + 1) / 2;
     if ((int64_t)(a.T / kTileRows + 1) * wide_tiles >= 2 * kUnits) {
