@@ -362,8 +362,8 @@ int moe_pre_attention(const moe_linear_shape* qkv_proj, const float* hidden, con
  * moe_validate_shape, moe_tile_bytes, moe_pages_required, moe_pack_weights, moe_unpack_weights, moe_page_table_validate, moe_combine,
  * moe_linear_pages_required and moe_linear_pack take such a shape, all others MOE_DTYPE_F32 or MOE_DTYPE_BF16 alone: router and
  * permutation take the bf16 shape with otherwise the same fields.
- * Sizes: H, F and a linear map's K multiples of 256 below 2^17, N a multiple of 128; T * H < 2^32.  A row's bits depend neither on how many
- * rows its call has nor on what they hold. */
+ * Sizes: H, F and a linear map's K multiples of 256 below 2^17, N a multiple of 128; T * H < 2^32.  A row that is quantised, normalised,
+ * multiplied or goes through an expert has the same bits whatever other rows its call has and whatever they hold. */
 
 /* Rows in 8 bits.  x: device, float or bf16 (x_dtype) [T][N], row t at x + t * row_elements; x_q: device int8[T][N]; x_scale: device
  * float[T].  N and row_elements multiples of 4, x aligned to four of its elements, x_q to 4 bytes; no two of them overlap. */
@@ -391,7 +391,8 @@ typedef struct moe_expert_scales {      /* device arrays */
  *   h[r] = bf16(silu(g) * u), g and u from W1_e and W3_e;  h_q[r], h_scale[r]: h[r] in 8 bits;  out[r] = bf16(row_w[r] * (W2_e h[r])).
  * x_q: device int8[T][H] with row_src (device int32[R]), else int8[R][H]; x_scale: float[T] or float[R]; h: device bf16[R][F];
  * h_q: device int8[R][F]; h_scale: device float[R]; out: device bf16[R][H]; row_w: device float[R] or NULL; status as for moe_expert_ffn.
- * x_q, h, h_q, out and the pool 16-byte aligned; none of what is written overlaps anything else. */
+ * Rows from offsets[E] on are left as they were.  x_q, h, h_q, out and the pool 16-byte aligned; none of what is written overlaps
+ * anything else. */
 int moe_expert_ffn_i8(const moe_shape* s, const int8_t* x_q, const float* x_scale, const int32_t* row_src, const int32_t* offsets,
                       const int32_t* page_table, const void* page_pool, int64_t pool_pages, const moe_expert_scales* scales,
                       const float* row_w, void* h, int8_t* h_q, float* h_scale, void* out, int32_t* status, void* stream);

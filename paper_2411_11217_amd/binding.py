@@ -706,6 +706,19 @@ def _optional(t, dtype, shape, name):
     return None if t is None else _dev(t, dtype, shape, name)
 
 
+def _here(*tensors):
+    """The kernels go to a stream of the current device: memory of another one is not theirs to read."""
+    now = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != now:
+            raise ValueError(f"a tensor is on device {t.get_device()}, the current device is {now}")
+
+
+@functools.lru_cache(maxsize=256)
+def _pages_per_expert(shape: bytes) -> int:      # a function of the sizes alone, by the bytes of the structure: shorter than reading its fields
+    return sum(pages_required(MoEShape.from_buffer_copy(shape)))
+
+
 def moe_quantize_i8(x, x_q: Optional[torch.Tensor] = None, x_scale: Optional[torch.Tensor] = None, stream=None):
     """x float32 or bf16 [T, N], elements of a row next to each other, N and the rows' distance multiples of 4
     -> (x_q int8 [T, N], x_scale float32 [T]); x_q * x_scale[:, None] stands for x."""
@@ -718,6 +731,7 @@ def moe_quantize_i8(x, x_q: Optional[torch.Tensor] = None, x_scale: Optional[tor
         raise TypeError(f"x: expected torch.float32 or torch.bfloat16, got {x.dtype}")
     if N > 1 and x.stride(1) != 1:
         raise ValueError("x: the elements of a row must be next to each other")
+    _here(x, x_q, x_scale)
     if x_q is None or x_scale is None:
         with _on(stream):
             x_q = torch.empty((T, N), dtype=torch.int8, device=x.device) if x_q is None else x_q
@@ -735,6 +749,7 @@ def moe_add_rmsnorm_i8(hidden, delta, gamma, eps: float, want_hidden: bool = Tru
     ph = _optional(hidden, torch.float32, (T, H), "hidden")
     pd = _dev(delta, torch.float32, (T, H), "delta")
     pg = _dev(gamma, torch.float32, (H,), "gamma")
+    _here(hidden, delta, gamma)
     dev = delta.device
     with _on(stream):
         hs = torch.empty_like(delta) if want_hidden else None                  # half as long as torch.empty
@@ -754,6 +769,7 @@ def moe_linear_i8(ls: LinearShape, x_q, x_scale, page_table, page_pool, w_scale,
     pp = _pool(page_pool, ls.page_bytes)
     pw = _dev(w_scale, torch.float32, (ls.N,), "w_scale")
     ps = _optional(status, torch.int32, (4,), "status")
+    _here(x_q, x_scale, page_table, page_pool, w_scale, status)
     with _on(stream):
         out = torch.empty((ls.T, ls.N), dtype=torch.float32, device=x_q.device)
     _check(_lib().moe_linear_i8(ctypes.byref(ls), px, pxs, pt, pp, int(page_pool.shape[0]), pw, out.data_ptr(), ps, _stream(stream)), "moe_linear_i8")
@@ -764,15 +780,15 @@ def moe_expert_ffn_i8(s: MoEShape, x_q, x_scale, offsets, page_table, page_pool,
     """x_q int8 [T, H] with row_src, else [R, H] -> (h_q int8 [R, F], h_scale float32 [R], out bf16 [R, H])"""
     R = s.R
     rows = R if row_src is None else s.T
-    gu, d = pages_required(s)
     px = _dev(x_q, torch.int8, (rows, s.H), "x_q")
     pxs = _dev(x_scale, torch.float32, (rows,), "x_scale")
     pr = _optional(row_src, torch.int32, (R,), "row_src")
     po = _dev(offsets, torch.int32, (s.E + 1,), "offsets")
-    pt = _dev(page_table, torch.int32, (s.E, gu + d), "page_table")
+    pt = _dev(page_table, torch.int32, (s.E, _pages_per_expert(bytes(s))), "page_table")
     pp = _pool(page_pool, s.page_bytes)
     pw = _optional(row_w, torch.float32, (R,), "row_w")
     ps = _optional(status, torch.int32, (4,), "status")
+    _here(x_q, x_scale, row_src, offsets, page_table, page_pool, row_w, status, scales.w1, scales.w3, scales.w2)
     with _on(stream):
         h_q = torch.empty((R, s.F), dtype=torch.int8, device=x_q.device)
         h = torch.empty_like(h_q, dtype=torch.bfloat16)
@@ -805,14 +821,14 @@ def moe_layer_i8(s: MoEShape, x, x_q, x_scale, Wr, page_table, page_pool, scales
                  y: Optional[torch.Tensor] = None, stream=None):
     """x bf16 [T, H] for the router, the same rows in 8 bits for the experts (both of moe_add_rmsnorm_i8)
     -> (y float32 [T, H], workspace uint8, its first int32 the status word)"""
-    gu, d = pages_required(s)
     px = _dev(x, torch.bfloat16, (s.T, s.H), "x")
     pq = _dev(x_q, torch.int8, (s.T, s.H), "x_q")
     pqs = _dev(x_scale, torch.float32, (s.T,), "x_scale")
     pw = _dev(Wr, torch.bfloat16, (s.E, s.H), "Wr")
     pb = _optional(bias, torch.float32, (s.E,), "bias")
-    pt = _dev(page_table, torch.int32, (s.E, gu + d), "page_table")
+    pt = _dev(page_table, torch.int32, (s.E, _pages_per_expert(bytes(s))), "page_table")
     pp = _pool(page_pool, s.page_bytes)
+    _here(x, x_q, x_scale, Wr, bias, page_table, page_pool, workspace, y, scales.w1, scales.w3, scales.w2)
     if workspace is None or y is None:
         with _on(stream):
             workspace = _scratch(layer_i8_workspace_bytes(s), x.device) if workspace is None else workspace
@@ -834,6 +850,7 @@ def moe_pre_attention_i8(qkv_proj: LinearShape, hidden, delta, norm_gamma, eps, 
     pp = _pool(page_pool, qkv_proj.page_bytes)
     pw = _dev(qkv_scale, torch.float32, (qkv_proj.N,), "qkv_scale")
     ps = _optional(status, torch.int32, (4,), "status")
+    _here(hidden, delta, norm_gamma, qkv_table, page_pool, qkv_scale, status)
     dev = delta.device
     with _on(stream):
         hidden_out = torch.empty(shape, dtype=torch.float32, device=dev)
@@ -854,7 +871,6 @@ def post_attention_i8_workspace_bytes(s: MoEShape, o_proj: LinearShape) -> int:
 def moe_post_attention_i8(s: MoEShape, o_proj: LinearShape, attn, hidden, o_table, o_scale, norm_gamma, eps, Wr, page_table, page_pool, scales: ExpertScales, bias=None,
                           workspace: Optional[torch.Tensor] = None, stream=None):
     """-> (hidden_mid float32, x_moe bf16, y float32, all [T, H], workspace uint8, its first int32 the status word)"""
-    gu, d = pages_required(s)
     pa = _dev(attn, torch.bfloat16, (s.T, o_proj.K), "attn")
     ph = _dev(hidden, torch.float32, (s.T, s.H), "hidden")
     po = _dev(o_table, torch.int32, (linear_pages_required(o_proj),), "o_table")
@@ -862,8 +878,9 @@ def moe_post_attention_i8(s: MoEShape, o_proj: LinearShape, attn, hidden, o_tabl
     pg = _dev(norm_gamma, torch.float32, (s.H,), "norm_gamma")
     pw = _dev(Wr, torch.bfloat16, (s.E, s.H), "Wr")
     pb = _optional(bias, torch.float32, (s.E,), "bias")
-    pt = _dev(page_table, torch.int32, (s.E, gu + d), "page_table")
+    pt = _dev(page_table, torch.int32, (s.E, _pages_per_expert(bytes(s))), "page_table")
     pp = _pool(page_pool, s.page_bytes)
+    _here(attn, hidden, o_table, o_scale, norm_gamma, Wr, bias, page_table, page_pool, workspace, scales.w1, scales.w3, scales.w2)
     dev = attn.device
     with _on(stream):
         hidden_mid = torch.empty((s.T, s.H), dtype=torch.float32, device=dev)

@@ -202,7 +202,7 @@ int moe_post_attention_i8(const moe_shape* s, const moe_linear_shape* o_proj, co
     char* ws = (char*)workspace;
     int8_t *a_q = (int8_t*)(ws + L.a_q), *x_q = (int8_t*)(ws + L.x_q);
     float *a_scale = (float*)(ws + L.a_scale), *x_scale = (float*)(ws + L.x_scale), *o = (float*)(ws + L.o);
-    rc = launch_quantize_i8(s->T, o_proj->K, attn, MOE_DTYPE_BF16, o_proj->K, a_q, a_scale, false, st);
+    rc = launch_quantize_i8(s->T, o_proj->K, attn, MOE_DTYPE_BF16, o_proj->K, a_q, a_scale, false, nullptr, st);
     if (rc != MOE_OK) return rc;
     rc = enqueue_linear(*o_proj, a_q, a_scale, o_table, page_pool, pool_pages, o_scale, o, nullptr, st);
     if (rc != MOE_OK) return rc;

@@ -392,6 +392,77 @@ def test_experts_bad_pages(T):
         status.zero_()
 
 
+def test_experts_rows_behind_the_last_expert_stay():
+    """offsets that end before R: the rows behind are neither computed nor written."""
+    x = Experts(512, 1024, 4, 2, 65536)
+    lib = B._lib()
+    for T in (5, 100, 900):
+        q, scale = x.rows(T)
+        offsets, row_src, row_w = x.routing(T)
+        cut = int(offsets[3])                    # the last expert has no rows now
+        offsets[4] = cut
+        R = 2 * T
+        dev = [t.cuda() for t in (q, scale, row_src, offsets, row_w)]
+        h_q, h_scale = torch.full((R, 1024), 77, dtype=torch.int8, device="cuda"), torch.full((R,), 5.0, device="cuda")
+        h, out = torch.full((R, 1024), NAN, dtype=torch.bfloat16, device="cuda"), torch.full((R, 512), 9.0, dtype=torch.bfloat16, device="cuda")
+        s = x.shape(T)
+        rc = lib.moe_expert_ffn_i8(B.ctypes.byref(s), dev[0].data_ptr(), dev[1].data_ptr(), dev[2].data_ptr(), dev[3].data_ptr(), x.table.data_ptr(), x.pool.data_ptr(), x.pool.shape[0],
+                                   x.dev.pointers(s), dev[4].data_ptr(), h.data_ptr(), h_q.data_ptr(), h_scale.data_ptr(), out.data_ptr(), None, B._stream(None))
+        assert rc == 0
+        assert (h_q[cut:] == 77).all() and (h_scale[cut:] == 5).all() and (out[cut:] == 9).all() and torch.isnan(h[cut:]).all()
+        x.check(q, scale, offsets, row_src, row_w, (h_q, h_scale, out), some=10)
+
+
+def test_experts_intermediates_beyond_32_bits():
+    """h of more than 2^32 bytes, h_q of more than 2^31: the last rows are as right as the first."""
+    T, x = 152000, Experts(256, 14336, 2, 1, 65536)
+    q, scale = x.rows(T)
+    ids = (torch.arange(T) >= T - 300).long()[:, None]
+    offsets, row_src, row_w = x.routing(T, ids)
+    assert T * 14336 > 2 ** 31
+    h_q, h_scale, out = x.run(T, q, scale, offsets, row_src, row_w)
+    rows = torch.tensor([0, 1, 70000, 149000, T - 301, T - 300, T - 256, T - 1])
+    few = torch.tensor([0, 5, 8], dtype=torch.int32)
+    got = [t[rows.cuda()] for t in (h_q, h_scale, out)]
+    token = row_src[rows].long()
+    x.check(q[token], scale[token], few, None, row_w[rows], got)
+
+
+@pytest.mark.parametrize("option", ["xcd_remap", "half_tiles", "tall_tiles", "tall_first", "chunked", "balance", "down_cols"])
+def test_options_change_no_bit(option):
+    x = Experts(256, 1280, 4, 1, 65536)
+    lin = Linear(256, 2176, 65536)
+    rows = {T: (x.rows(T), x.routing(T)) for T in (40, 700, 1500)}
+    lin_rows = lin.rows(1500)
+
+    def all_of_it():
+        return [t for T, (r, p) in rows.items() for t in x.run(T, *r, *p)] + [lin.run(*lin_rows)]
+
+    want, value = all_of_it(), M.get_option(option)
+    try:
+        for v in {"chunked": (0, 8), "down_cols": (1, 2)}.get(option, (0,)):
+            M.set_option(option, v)
+            assert all(torch.equal(a, b) for a, b in zip(want, all_of_it())), v
+    finally:
+        M.set_option(option, value)
+
+
+def test_more_rows_than_blocks():
+    """Rows beyond 2^20 blocks are taken in turn."""
+    T = (1 << 20) + 77
+    x = torch.randn((4 * T, 4), device="cuda")
+    q, scale = M.moe_quantize_i8(x)
+    rows = torch.tensor([0, 1, T - 1, 4 * (1 << 20) - 1, 4 * (1 << 20), 4 * (1 << 20) + 5, 4 * T - 1])
+    check_quantized(x.cpu()[rows], q.cpu()[rows], scale.cpu()[rows])
+    y = torch.randn((T, 520), device="cuda").to(torch.bfloat16)
+    q, scale = M.moe_quantize_i8(y)
+    rows = torch.tensor([0, T - 78, T - 77, T - 1])
+    check_quantized(y[rows.cuda()].cpu(), q[rows.cuda()], scale[rows.cuda()])
+    delta, gamma = torch.randn((T, 260), device="cuda"), torch.ones(260, device="cuda")
+    got = M.moe_add_rmsnorm_i8(None, delta, gamma, 1e-5)
+    check_norm(None, delta[rows.cuda()].cpu(), gamma.cpu(), 1e-5, [t[rows.cuda()] for t in got])
+
+
 # ---------------------------------------------------------------------------- together
 
 def layer_inputs(T, H=512, F=768, E=4, k=2, seed=0, K=None):

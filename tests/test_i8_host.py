@@ -261,6 +261,17 @@ def test_binding_checks_before_the_library():
         M.make_linear_shape(3, 256, 128, 65536, "f32")
 
 
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class On:
+        def __init__(self, device):
+            self.get_device = lambda: device
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    B._here(On(1), None, On(1))
+    with pytest.raises(ValueError, match="device 0, the current device is 1"):
+        B._here(On(1), None, On(0))
+
+
 # ---------------------------------------------------------------------------- the oracle
 
 def test_oracle_quantize():
