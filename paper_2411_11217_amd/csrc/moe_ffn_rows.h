@@ -156,7 +156,7 @@ __global__ __launch_bounds__(64 * CW * RG * KG) void ffn_rows(const GemmParams p
         tiles_mine = NT;
         // Integers, blocks of few columns: rows that the tile does not have are zeros instead of its last row again (us, in a graph: 4096 x 6144 1 row 8.7 / 7.9, 36: 10.8 / 10.1; blocks
         // of 64 columns, 100 rows 12.9 / 13.2, which are left as they were).
-        constexpr bool kSkip = Op::kScaled && RG > 1;
+        constexpr bool kSkip = Op::kScaled && (RG > 1 || BM == 32);
         i32x4 areg[D][NA], breg[D][2][NB];
         if constexpr (kSkip)
 #pragma unroll
