@@ -37,7 +37,7 @@ HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-pthread", "-Wall", "-I", os.path.j
 # has no need to; this check of the assembly the compiler generates makes a build fail if it ever does, or if such a
 # kernel spills to scratch memory.  The kernels' own uses print as a[N] or a[N:M], the allocator's as aN.
 ACCUMULATOR_OWNERS = {"moe_ffn_bf16.hip", "moe_ffn_halves_bf16.hip", "moe_ffn_narrow_bf16.hip", "moe_ffn_gate_i8.hip", "moe_ffn_gate_halves_i8.hip", "moe_ffn_down_i8.hip",
-                      "moe_ffn_down_halves_i8.hip", "moe_ffn_narrow_i8.hip", "moe_ffn_linear_i8.hip", "moe_ffn_linear_narrow_i8.hip"}
+                      "moe_ffn_narrow_i8.hip", "moe_ffn_linear_i8.hip", "moe_ffn_linear_narrow_i8.hip"}
 
 
 def check_kernel_assembly(asm_path: str) -> None:

@@ -285,12 +285,11 @@ bool thin_takes_down(const moe_shape& s, int k);
 int launch_gate_up_thin_bf16(GemmParams& p, int F, int R, int n_exp, hipStream_t st);
 int launch_down_thin_bf16(GemmParams& p, int H, int R, int n_exp, hipStream_t st);
 
-// the launches of the 256-row blocks (moe_ffn_gemm.h) with 8-bit integers: gate/up and down whole or with their last round in halves, the
+// the launches of the 256-row blocks (moe_ffn_gemm.h) with 8-bit integers: gate/up whole or with its last round in halves, down with it, the
 // down launch with 128-wide column tiles, whole or 64-wide in the last round; the linear map
 int launch_gate_up_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
 int launch_gate_up_halves_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
 int launch_down_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
-int launch_down_halves_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
 int launch_down_narrow_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
 int launch_down_narrow_halves_i8(const GemmParams& p, int R, int n_exp, hipStream_t st);
 int launch_linear_wide_i8(const GemmParams& p, int T, hipStream_t st);
