@@ -48,9 +48,9 @@ def gate_up_kernel(cfg):
     if cfg.dtype == "f32":
         return "ffn_split_f32<0>" if each > 32 or (each > 16 and cfg.F // 64 * cfg.E >= 256) else "ffn_few_rows_f32<0>"
     if each > 80:
-        return "ffn_gemm_bf16<0>"
+        return "ffn_gemm<Bf16, 0>"
     experts = cfg.E * (1.0 - (1.0 - cfg.k / cfg.E) ** cfg.T)       # with rows, on average
-    return "ffn_thin_bf16<0>" if cfg.T <= 16 and experts * (cfg.F // 64) <= 440 else "ffn_rows_bf16<0>"
+    return "ffn_thin<Bf16, 0>" if cfg.T <= 16 and experts * (cfg.F // 64) <= 440 else "ffn_rows<Bf16, 0>"
 
 
 def main():
