@@ -28,6 +28,33 @@ constexpr int kFewRows = 96;
 // tokens 28 / 30 | 28 / 31, six layers 32 / 31.  Mixtral-8x7B shape 64 tokens 255 / 231, 256: 288 / 252, 1000: 421 / 389.
 constexpr int64_t kHintBytes = (int64_t)128 << 20;
 
+// Blocks of the kernel for few rows: 64 rows up to kRows64Max per expert on average, else 128.  Features per block: 128, which read the rows half as often as 64, where these are blocks enough.  us for the
+// call, 64 / 128: 2048 x 4096 160 tokens (256 blocks of 128) 53.6 / 52.4, 64 experts of 2048 x 1024 320 tokens 87.0 / 85.3, 1024 x 2816 64 tokens 31.4 / 30.3, 5 experts of 1280 x 768 (30) 26 tokens 18.1 / 20.3, 133: 23.8 / 24.8.
+//   With more than kRows64Max rows 112 where a compute unit then has less to read: it has weights from HBM at 25 GB/s whatever the others do, so the one with the most blocks is what the launch waits for.  112 / 128:
+// Mixtral-8x7B shape 256 tokens (1024 blocks, four to a compute unit / 896, three and a half) 245.6 / 249.2, DBRX shape 320 tokens (six / five and a quarter) 551 / 558, but 2048 x 4096 256 tokens (296 / 256) 67.4 / 56.0.
+static int launch_gate_up_few(GemmParams& p, const moe_shape& s, int R, int rows_each, hipStream_t st) {
+    const int64_t groups = s.F / 16;
+    const bool tall = rows_each > kRows64Max;
+    if (s.E * (groups / 8) < (tall ? 64 : 128)) return tall ? launch_rows<ToFloat, 0, 8, 4, 1, 1, 2>(p, s.F, R, s.E, st) : launch_rows<ToFloat, 0, 4, 4, 1, 1, 4>(p, s.F, R, s.E, st);
+    if (!tall) return launch_rows<ToFloat, 0, 4, 8, 1, 1, 4>(p, s.F, R, s.E, st);
+    auto longest = [&](int cw) { return (s.E * ((groups + cw - 1) / cw) + kUnits - 1) / kUnits * (2 * cw + 1); };      // half a group's time for the rows
+    return longest(7) < longest(8) ? launch_rows<ToFloat, 0, 8, 7, 1, 1, 2>(p, s.F, R, s.E, st) : launch_rows<ToFloat, 0, 8, 8, 1, 1, 2>(p, s.F, R, s.E, st);
+}
+
+// Columns per block: 128, or 64 or 32 where they still make one round and 128 leave compute units without a block.  us for the call, 128 / 64 / 32: 2048 x 4096 64 tokens (128 blocks of 128) 47.9 / 44.8 / 44.6, 256: 56.3 / 52.7 /
+// 57.6; 1024 x 2816 64 tokens (64) 31.3 / 28.7 / 28.1, 256: 36.6 / 34.9 / 34.4; 5 experts of 1280 x 768 66 tokens (50) 20.3 / 19.6 / 19.6, but 106 tokens (128 rows to a block, six k-steps) 24.2 / 24.9 / 25.2; Mixtral-8x7B shape 64 (256)
+// 230 / 231 / 233, 256: 250 / 263 / 293.
+static int launch_down_few(GemmParams& p, const moe_shape& s, int R, int rows_each, hipStream_t st) {
+    const int64_t blocks = (int64_t)s.E * (s.H / 128);
+    if (rows_each > kRows64Max) {
+        if (2 * blocks <= kUnits && p.KT >= 12) return launch_rows<ToBf16, 1, 8, 4, 1, 1, 4>(p, s.H, R, s.E, st);
+        return launch_rows<ToBf16, 1, 8, 8, 1, 1, 4>(p, s.H, R, s.E, st);
+    }
+    if (4 * blocks <= kUnits) return launch_rows<ToBf16, 1, 4, 2, 1, 1, 4>(p, s.H, R, s.E, st);
+    if (2 * blocks <= kUnits) return launch_rows<ToBf16, 1, 4, 4, 1, 1, 4>(p, s.H, R, s.E, st);
+    return launch_rows<ToBf16, 1, 4, 8, 1, 1, 4>(p, s.H, R, s.E, st);
+}
+
 int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st) {
     const int R = s.T * s.k, rows_each = R / s.E;
     const Geom g = geometry(s);
@@ -58,7 +85,7 @@ int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st)
         return last != 0 && last <= kUnits / 2;
     };
     int rc = !few ? (half_round() ? launch_gate_up_halves_i8(p, R, s.E, st) : launch_gate_up_i8(p, R, s.E, st))
-             : thin_takes_gate_up(s) ? launch_thin<ToFloat, 0, 2>(p, s.F, R, s.E, st) : gate_up_rows<ToFloat>(p, s.F, R, rows_each, s.E, st);
+             : thin_takes_gate_up(s) ? launch_thin<ToFloat, 0, 2>(p, s.F, R, s.E, st) : launch_gate_up_few(p, s, R, rows_each, st);
     if (rc != MOE_OK) return rc;
     rc = launch_quantize_i8(R, s.F, a.h, MOE_DTYPE_BF16, s.F, a.h_q, a.h_scale, p.stream != 0, a.offsets + s.E, st);
     if (rc != MOE_OK) return rc;
@@ -67,7 +94,7 @@ int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st)
     p.a_scale = a.h_scale;
     p.w_scale = a.scales.w2;
     p.row_w = a.row_w;
-    if (few) return thin_takes_down(s, s.F / 2) ? launch_thin<ToBf16, 1, 1>(p, s.H, R, s.E, st) : down_rows<ToBf16>(p, s.H, R, rows_each, s.E, st);
+    if (few) return thin_takes_down(s, s.F / 2) ? launch_thin<ToBf16, 1, 1>(p, s.H, R, s.E, st) : launch_down_few(p, s, R, rows_each, st);
     const int opt = get_opt(OPT_DOWN_COLS);
     const int64_t narrow_tiles = s.E * row_tiles_each * g.dt;
     if (opt == 1 || (opt == 0 && narrow_tiles <= kUnits)) {

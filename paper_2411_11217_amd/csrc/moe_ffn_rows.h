@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64 * CW * RG * KG) void ffn_rows(const GemmParams p
     constexpr int BM = 16 * RT, NB = MODE == 0 ? 2 * FC : FC, kCols = 16 * CW * FC;
     constexpr int kPass = 8 * CW * RG;               // rows that one load instruction per thread fetches
     constexpr int AJ = (BM + kPass - 1) / kPass, kStage = AJ * kPass * 128;
-    static_assert(RT % 2 == 0 && RT <= 8 && (128 % kCols == 0 || (MODE == 1 && FC == 1)) && (kPass <= BM || RG == 1 || kPass >= 16 * RG), "");
+    static_assert(RT % 2 == 0 && RT <= 8 && (128 % kCols == 0 || FC == 1) && (kPass <= BM || RG == 1 || kPass >= 16 * RG), "");
     constexpr int kOutRow = kCols * 2 + 16;          // MODE 0: bytes of a row of h in LDS, 16 of padding
     constexpr int kTeam = CW * RG, kPartial = kTeam * ((RT + RG - 1) / RG) * NB * 1024;      // wavefronts of a team, bytes of its sums
     constexpr int kSmem = MODE == 0 && BM * kOutRow > 2 * kStage ? BM * kOutRow : KG * 2 * kStage;
@@ -90,12 +90,12 @@ __global__ __launch_bounds__(64 * CW * RG * KG) void ffn_rows(const GemmParams p
         }
         return p.pool + (int64_t)slot * p.page_bytes;
     };
-    // MODE 1 with FC = 1: each wavefront has the page tile of its own 16 columns (a block may begin in one and end in the next)
-    constexpr bool kOwn = MODE == 1 && FC == 1;
+    // MODE 1 with FC = 1, and columns that are no part of a page tile: each wavefront has the page tile of its own 16 columns (a block may begin in one and end in the next)
+    constexpr bool kOwn = FC == 1 && (MODE == 1 || 128 % kCols != 0);
     constexpr int kColTiles = kOwn ? 1 : 128 / kCols;     // blocks per page tile along the columns
     const int group = kOwn ? min(nt * CW + cw, p.n_cols / 16 - 1) : 0;       // the last block may have wavefronts too many
     {
-        const int t0 = (kOwn ? (group >> 3) * p.KT : (nt / kColTiles) * (MODE == 0 ? 2 : 1) * p.KT) + k0;
+        const int t0 = (kOwn ? (group >> 3) * (MODE == 0 ? 2 : 1) * p.KT : (nt / kColTiles) * (MODE == 0 ? 2 : 1) * p.KT) + k0;
         page = t0 / p.tpp;
         within = t0 - page * p.tpp;
         tile[0] = page_addr(page) + (int64_t)within * kTileBytes;
@@ -270,6 +270,7 @@ __global__ __launch_bounds__(64 * CW * RG * KG) void ffn_rows(const GemmParams p
         auto store_rows = [&](auto past_l2) __attribute__((always_inline)) {
             for (int c = tid; c < rows_here * kChunks; c += 64 * CW * RG) {
                 const int row = c / kChunks, ch = c % kChunks;
+                if (kOwn && nt * kCols + ch * 8 >= p.n_cols) continue;       // of a wavefront too many
                 const i32x4 hv = *(const i32x4*)(smem + row * kOutRow + ch * 16);
                 i32x4* dst = (i32x4*)(o + (int64_t)row * p.ldo * 2 + ch * 16);
                 if constexpr (decltype(past_l2)::value) {

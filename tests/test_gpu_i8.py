@@ -354,14 +354,16 @@ def test_experts_rows_are_their_own(T):
         assert torch.equal(a.cpu()[of_bad], b.cpu()[of_bad])
 
 
-def test_experts_rows_have_the_same_bits_in_every_kernel():
-    """1, 30, 75 and up to 1000 rows per expert on average are the kernels for a handful of tokens, for few rows (two blocks), and blocks of 256 rows (halved, narrow)."""
-    x = Experts(512, 1024, 2, 1, 65536)
-    q, scale = x.rows(2000)
-    ids = torch.randint(0, 2, (2000, 1), generator=x.g)
+@pytest.mark.parametrize("H,F,E", [(512, 1024, 2), (256, 2816, 8), (256, 14336, 8), (2048, 512, 8)])
+def test_experts_rows_have_the_same_bits_in_every_kernel(H, F, E):
+    """Up to 2, 30, 75 and up to 1000 rows per expert on average are the kernels for a handful of tokens, for few rows (64 and 128, in blocks of 64, 112 and 128 features and of
+    32, 64 and 128 columns by the size), and blocks of 256 rows (halved, narrow)."""
+    x = Experts(H, F, E, 1, 65536)
+    q, scale = x.rows(1000 * E)
+    ids = torch.randint(0, E, (1000 * E, 1), generator=x.g)
     ids[:3] = torch.tensor([[0], [1], [0]])
     first = None
-    for T in (3, 60, 150, 300, 900, 2000):
+    for T in (3, 30 * E, 60 * E, 75 * E, 150 * E, 450 * E, 1000 * E):
         offsets, row_src, _ = x.routing(T, ids[:T])
         got = x.run(T, q[:T], scale[:T], offsets, row_src, None)
         at = [int((row_src == t).nonzero()) for t in range(3)]
