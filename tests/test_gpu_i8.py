@@ -533,6 +533,23 @@ def test_no_tokens():
     assert M.moe_layer_i8(s, rows, q, scale, torch.zeros((4, 256), dtype=torch.bfloat16, **z), x.table, x.pool, x.dev)[0].shape == (0, 256)
 
 
+def test_two_layers_at_once():
+    """Two calls on two streams, each with its own workspace and both on the same weights, many times over each other."""
+    x, delta, gamma, Wr = layer_inputs(700, seed=5)
+    s = x.shape(700)
+    inputs = [M.moe_add_rmsnorm_i8(None, delta * f, gamma, 1e-5)[1:] for f in (1.0, -0.5)]
+    want = [M.moe_layer_i8(s, *i, Wr, x.table, x.pool, x.dev)[0].clone() for i in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    spaces = [torch.empty(M.layer_i8_workspace_bytes(s), dtype=torch.uint8, device="cuda") for _ in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for n, st in enumerate(streams):
+            got[n].append(M.moe_layer_i8(s, *inputs[n], Wr, x.table, x.pool, x.dev, workspace=spaces[n], stream=st)[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, w) for ys, w in zip(got, want) for y in ys)
+
+
 def test_on_a_stream_of_its_own_and_in_a_graph():
     """The whole run, residual to layer, on another stream and captured; replays with new inputs between eager calls give the eager bits."""
     T = 70
