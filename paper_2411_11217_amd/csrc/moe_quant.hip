@@ -148,7 +148,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel
 
 template <class In, int VEC, int WAVES, int PER>
 int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, hipStream_t st) {
-    const dim3 grid(std::min(WAVES == 1 ? (T + 3) / 4 : T, kMostBlocks)), block(WAVES == 1 ? 256 : 64 * WAVES);
+    const dim3 grid(std::min(WAVES == 1 ? T / 4 + (T % 4 != 0) : T, kMostBlocks)), block(WAVES == 1 ? 256 : 64 * WAVES);
     const bool far = (int64_t)T * pieces * VEC * ((int)sizeof(In) + 1) > kQuantizeFar;
     if (past) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, true>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live);
     else if (far) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live);
