@@ -406,8 +406,8 @@ int moe_layer_i8(const moe_shape* s, const void* x, const int8_t* x_q, const flo
 
 /* moe_pre_attention and moe_post_attention in 8 bits.  Pre: hidden_out = hidden + delta, x_q and x_scale its norm in 8 bits,
  * qkv = the projection (float[T][N]).  Post: attn (device bf16[T][o_proj->K]) in 8 bits, O projection, residual and norm (hidden_mid,
- * x_moe bf16, and in 8 bits in the workspace), moe_layer_i8.  (As in moe_post_attention an entry of o_table outside the pool is read as
- * page 0 and not reported.)  workspace: device, 256-byte aligned, the layer's at its start. */
+ * x_moe bf16, and in 8 bits in the workspace), moe_layer_i8.  workspace: device, 256-byte aligned, the layer's at its start; its status
+ * word reports entries of o_table outside the pool (read as page 0) as it does those of page_table. */
 int moe_pre_attention_i8(const moe_linear_shape* qkv_proj, const float* hidden, const float* delta, const float* norm_gamma, float eps,
                          const int32_t* qkv_table, const void* page_pool, int64_t pool_pages, const float* qkv_scale, float* hidden_out,
                          int8_t* x_q, float* x_scale, float* qkv, int32_t* status, void* stream);

@@ -2,6 +2,8 @@
 // Pure HBM traffic (read R*H floats, or bf16 behind 8-bit products, write T*H floats): one block per token,
 // four elements at a time along the row, the k rows of a token summed in slot order so the
 // result does not depend on scheduling.
+#include <type_traits>
+
 #include "moe_internal.h"
 
 namespace moe {
@@ -15,8 +17,10 @@ __device__ __forceinline__ float4 as_floats(const uint2& v) {        // four bf1
 template <class Four>
 __global__ __launch_bounds__(256) void combine_kernel(const Four* __restrict__ out, const int32_t* __restrict__ row_of,
                                                       const float* __restrict__ topk_w, int k, int R, int row_vec,
-                                                      float4* __restrict__ y) {
+                                                      float4* __restrict__ y, const int32_t* __restrict__ found, int32_t* __restrict__ status) {
     const int t = blockIdx.x;
+    if constexpr (std::is_same<Four, uint2>::value)
+        if (found && t == 0 && threadIdx.x == 0 && found[0]) atomicOr(status, found[0]);
     __shared__ int32_t rows[MOE_MAX_EXPERTS];
     __shared__ float wts[MOE_MAX_EXPERTS];
     if (threadIdx.x < k) {
@@ -42,11 +46,11 @@ __global__ __launch_bounds__(256) void combine_kernel(const Four* __restrict__ o
 }  // namespace
 
 int launch_combine(const moe_shape& s, const void* out, const int32_t* row_of, const float* topk_w, float* y,
-                   hipStream_t st) {
+                   hipStream_t st, const int32_t* found, int32_t* status) {
     if (s.dtype == MOE_DTYPE_I8)
-        hipLaunchKernelGGL(combine_kernel<uint2>, dim3(s.T), dim3(256), 0, st, (const uint2*)out, row_of, topk_w, s.k, s.T * s.k, s.H / 4, (float4*)y);
+        hipLaunchKernelGGL(combine_kernel<uint2>, dim3(s.T), dim3(256), 0, st, (const uint2*)out, row_of, topk_w, s.k, s.T * s.k, s.H / 4, (float4*)y, found, status);
     else
-        hipLaunchKernelGGL(combine_kernel<float4>, dim3(s.T), dim3(256), 0, st, (const float4*)out, row_of, topk_w, s.k, s.T * s.k, s.H / 4, (float4*)y);
+        hipLaunchKernelGGL(combine_kernel<float4>, dim3(s.T), dim3(256), 0, st, (const float4*)out, row_of, topk_w, s.k, s.T * s.k, s.H / 4, (float4*)y, nullptr, nullptr);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }

@@ -65,7 +65,7 @@ Layout layout(const moe_shape& s) {
 }
 
 int enqueue_layer(const moe_shape& s, const void* x, const int8_t* x_q, const float* x_scale, const void* Wr, const float* bias, const int32_t* page_table,
-                  const void* pool, int64_t pool_pages, const moe_expert_scales& scales, float* y, char* ws, hipStream_t st) {
+                  const void* pool, int64_t pool_pages, const moe_expert_scales& scales, float* y, char* ws, hipStream_t st, const int32_t* found = nullptr) {
     const Layout L = layout(s);
     const moe_shape r = routed(s);
     int32_t *status = (int32_t*)(ws + L.status), *ids = (int32_t*)(ws + L.ids), *offsets = (int32_t*)(ws + L.offsets), *row_src = (int32_t*)(ws + L.row_src),
@@ -84,14 +84,14 @@ int enqueue_layer(const moe_shape& s, const void* x, const int8_t* x_q, const fl
                       ws + L.out, status};
     rc = launch_expert_ffn_i8(s, a, st);
     if (rc != MOE_OK) return rc;
-    return launch_combine(s, ws + L.out, row_of, nullptr, y, st);
+    return launch_combine(s, ws + L.out, row_of, nullptr, y, st, found, status);
 }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// [the layer's workspace][attn in 8 bits][its scales][O projection, float [T][H]][x_moe in 8 bits][its scales]
+// [the layer's workspace][attn in 8 bits][its scales][O projection, float [T][H]][x_moe in 8 bits][its scales][the O projection's status words]
 struct PostLayout {
-    size_t a_q, a_scale, o, x_q, x_scale, total;
+    size_t a_q, a_scale, o, x_q, x_scale, found, total;
 };
 PostLayout post_layout(const moe_shape& s, int32_t K) {
     PostLayout L;
@@ -101,7 +101,8 @@ PostLayout post_layout(const moe_shape& s, int32_t K) {
     L.o = L.a_scale + up256(T * 4);
     L.x_q = L.o + up256(T * s.H * 4);
     L.x_scale = L.x_q + up256(T * s.H);
-    L.total = L.x_scale + up256(T * 4);
+    L.found = L.x_scale + up256(T * 4);
+    L.total = L.found + 256;
     return L;
 }
 
@@ -202,13 +203,15 @@ int moe_post_attention_i8(const moe_shape* s, const moe_linear_shape* o_proj, co
     char* ws = (char*)workspace;
     int8_t *a_q = (int8_t*)(ws + L.a_q), *x_q = (int8_t*)(ws + L.x_q);
     float *a_scale = (float*)(ws + L.a_scale), *x_scale = (float*)(ws + L.x_scale), *o = (float*)(ws + L.o);
-    rc = launch_quantize_i8(s->T, o_proj->K, attn, MOE_DTYPE_BF16, o_proj->K, a_q, a_scale, false, nullptr, st);
+    // The router clears the layer's status words behind the O projection, which therefore has its own: cleared with attn's rows, joined to the others by the combine.
+    int32_t* const found = (int32_t*)(ws + L.found);
+    rc = launch_quantize_i8(s->T, o_proj->K, attn, MOE_DTYPE_BF16, o_proj->K, a_q, a_scale, false, nullptr, st, found);
     if (rc != MOE_OK) return rc;
-    rc = enqueue_linear(*o_proj, a_q, a_scale, o_table, page_pool, pool_pages, o_scale, o, nullptr, st);
+    rc = enqueue_linear(*o_proj, a_q, a_scale, o_table, page_pool, pool_pages, o_scale, o, found, st);
     if (rc != MOE_OK) return rc;
     rc = launch_add_rmsnorm_i8(s->T, s->H, hidden, o, norm_gamma, eps, hidden_mid, x_moe, x_q, x_scale, st);
     if (rc != MOE_OK) return rc;
-    return enqueue_layer(*s, x_moe, x_q, x_scale, Wr, bias, page_table, page_pool, pool_pages, *scales, y, ws, st);
+    return enqueue_layer(*s, x_moe, x_q, x_scale, Wr, bias, page_table, page_pool, pool_pages, *scales, y, ws, st, found);
 }
 
 }  // extern "C"

@@ -118,7 +118,7 @@ struct FfnI8Args {
 };
 int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st);
 int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live,
-                       hipStream_t st);          // past: q past the L2; live: device, or null: rows from *live on are left as they were
+                       hipStream_t st, int32_t* clear = nullptr);      // past: q past the L2; live: device, or null: rows from *live on are left as they were; clear: four words set to zero
 bool norm_takes(int32_t H, float eps);
 int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* q, float* scale,
                           hipStream_t st);
@@ -126,7 +126,8 @@ int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta,
 int launch_cast_bf16(int64_t n, const float* in, void* out, hipStream_t st);
 int launch_linear_bf16(const LinearArgs& a, hipStream_t st);
 
+// found, status: with MOE_DTYPE_I8 the error bits in found[0] join status[0] (found may be null)
 int launch_combine(const moe_shape& s, const void* out, const int32_t* row_of, const float* topk_w,
-                   float* y, hipStream_t st);
+                   float* y, hipStream_t st, const int32_t* found = nullptr, int32_t* status = nullptr);
 
 }  // namespace moe

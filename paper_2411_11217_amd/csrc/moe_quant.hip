@@ -96,16 +96,17 @@ struct Piece<uint16_t, 8> {
 
 constexpr int kMostBlocks = 1 << 20;             // rows beyond theirs are taken in turn
 
-// live: device, or null: rows from *live on are left as they were.  WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is read twice.
+// live: device, or null: rows from *live on are left as they were.  clear: four words set to zero, or null.  WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is read twice.
 template <class In, int VEC, int WAVES, int PER, bool FAR, bool PAST>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel(const In* __restrict__ x, int64_t row_elements, int T, int pieces, int8_t* __restrict__ q,
-                                                                                 float* __restrict__ scale, const int32_t* __restrict__ live) {
+                                                                                 float* __restrict__ scale, const int32_t* __restrict__ live, int32_t* __restrict__ clear) {
     typedef Piece<In, VEC> P;
     __shared__ uint32_t part[WAVES];
     constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = 64 * WAVES;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int me = WAVES == 1 ? lane : threadIdx.x;
     const int rows = live ? min(T, *live) : T;   // wanted at the first store only
+    if (clear && blockIdx.x == 0 && threadIdx.x < 4) clear[threadIdx.x] = 0;
     for (int64_t t = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); t < T; t += (int64_t)gridDim.x * kRows) {
         const In* const row = x + t * row_elements;
         int8_t* const out = q + t * pieces * VEC;
@@ -147,12 +148,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel
 }
 
 template <class In, int VEC, int WAVES, int PER>
-int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, hipStream_t st) {
+int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, int32_t* clear, hipStream_t st) {
     const dim3 grid(std::min(WAVES == 1 ? T / 4 + (T % 4 != 0) : T, kMostBlocks)), block(WAVES == 1 ? 256 : 64 * WAVES);
     const bool far = (int64_t)T * pieces * VEC * ((int)sizeof(In) + 1) > kQuantizeFar;
-    if (past) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, true>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live);
-    else if (far) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live);
-    else hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, false, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live);
+    if (past) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, true>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
+    else if (far) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
+    else hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, false, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }
@@ -160,15 +161,15 @@ int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t
 // Wavefronts by the length of the row alone: a row's loads are then under way at once, and what is in flight fills the chip.  us, 256 threads to
 // every row / these: 512 x 14336 9.1 / 5.9, 8192 x 14336 88 / 64, 60000 x 256 53 / 17, 1 x 28672 10.4 / 3.2.
 template <class In, int VEC>
-int launch_quantize(int T, int N, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, hipStream_t st) {
+int launch_quantize(int T, int N, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, int32_t* clear, hipStream_t st) {
     const int pieces = N / VEC;
-    if (pieces <= 64) return launch_quantize<In, VEC, 1, 1>(T, pieces, x, row_elements, q, scale, past, live, st);
-    if (pieces <= 128) return launch_quantize<In, VEC, 1, 2>(T, pieces, x, row_elements, q, scale, past, live, st);
-    if (pieces <= 512) return launch_quantize<In, VEC, 4, 2>(T, pieces, x, row_elements, q, scale, past, live, st);
-    if (pieces <= 1024) return launch_quantize<In, VEC, 8, 2>(T, pieces, x, row_elements, q, scale, past, live, st);
-    if (pieces <= 2048) return launch_quantize<In, VEC, 16, 2>(T, pieces, x, row_elements, q, scale, past, live, st);
-    if (pieces <= 4096) return launch_quantize<In, VEC, 16, 4>(T, pieces, x, row_elements, q, scale, past, live, st);
-    return launch_quantize<In, VEC, 16, 0>(T, pieces, x, row_elements, q, scale, past, live, st);
+    if (pieces <= 64) return launch_quantize<In, VEC, 1, 1>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    if (pieces <= 128) return launch_quantize<In, VEC, 1, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    if (pieces <= 512) return launch_quantize<In, VEC, 4, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    if (pieces <= 1024) return launch_quantize<In, VEC, 8, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    if (pieces <= 2048) return launch_quantize<In, VEC, 16, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    if (pieces <= 4096) return launch_quantize<In, VEC, 16, 4>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    return launch_quantize<In, VEC, 16, 0>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
 }
 
 // Residual and norm: one pass over the rows.  s = hidden + delta stays in registers, its squares are added up, then the magnitudes of y are
@@ -266,10 +267,10 @@ int launch_norm(const NormArgs& a, hipStream_t st) {
 
 namespace moe {
 
-int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, hipStream_t st) {
-    if (x_dtype == MOE_DTYPE_F32) return launch_quantize<float, 4>(T, N, (const float*)x, row_elements, q, scale, past, live, st);
-    if (N % 8 == 0 && row_elements % 8 == 0 && aligned16(x) && (uintptr_t)q % 8 == 0) return launch_quantize<uint16_t, 8>(T, N, (const uint16_t*)x, row_elements, q, scale, past, live, st);
-    return launch_quantize<uint16_t, 4>(T, N, (const uint16_t*)x, row_elements, q, scale, past, live, st);
+int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, hipStream_t st, int32_t* clear) {
+    if (x_dtype == MOE_DTYPE_F32) return launch_quantize<float, 4>(T, N, (const float*)x, row_elements, q, scale, past, live, clear, st);
+    if (N % 8 == 0 && row_elements % 8 == 0 && aligned16(x) && (uintptr_t)q % 8 == 0) return launch_quantize<uint16_t, 8>(T, N, (const uint16_t*)x, row_elements, q, scale, past, live, clear, st);
+    return launch_quantize<uint16_t, 4>(T, N, (const uint16_t*)x, row_elements, q, scale, past, live, clear, st);
 }
 
 int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* q, float* scale,
