@@ -80,8 +80,8 @@ class DecodeLayers:
     def step(self, embedded: torch.Tensor, fresh: torch.Tensor) -> Tuple[torch.Tensor, B.KvStep]:
         """embedded float32 [T, H]: the fresh tokens of all requests, in the order of the requests; fresh int32 [n_requests].
         -> (hidden states float32 [T, H] after the last layer, the step's tables).  Nothing waits for the device: a request that does
-        not fit (bits 1 and 2 of status[0]) keeps its length, and its rows of the result mean nothing.  The tables are written again two
-        steps later.  A call that raises leaves the requests as they were, and the step can be taken again."""
+        not fit (bits 1 and 2 of status[0]) keeps its length, and its rows of the result mean nothing.  Entries of page tables outside their
+        pool set bit 0, of the weights' tables with 8-bit weights only.  The tables are written again two steps later.  A call that raises leaves the requests as they were, and the step can be taken again."""
         kv, T = self.kv, embedded.shape[0]
         if T != self._rows:
             self._rows, self._pair = T, [B.KvStep(kv, self.n_requests, T, embedded.device) for _ in range(2)]
@@ -93,8 +93,14 @@ class DecodeLayers:
         s = self.shape.with_tokens(T)
         qkv_proj = B.make_linear_shape(T, s.H, self.qkv_width, s.page_bytes, s.dtype)
         o_proj = B.make_linear_shape(T, self.attn_width, s.H, s.page_bytes, s.dtype)
+        space = None
+        if s.dtype == B.DTYPE_I8:
+            # One buffer for the layers' workspaces, each of which begins 256 bytes behind the one before: a layer writes over what is behind the beginnings of
+            # those before it, whose status words so stay until the end of the step, where they are looked at all at once.
+            need = B.post_attention_i8_workspace_bytes(s, o_proj)
+            space = B._scratch(need + 256 * len(self.layers), embedded.device)
         hidden, delta = None, embedded
-        for w, (k_cache, v_cache) in zip(self.layers, self.caches):
+        for i, (w, (k_cache, v_cache)) in enumerate(zip(self.layers, self.caches)):
             if w.scales is None:
                 hidden, _, qkv, _ = B.moe_pre_attention(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, want_bf16=False)
             else:
@@ -107,8 +113,10 @@ class DecodeLayers:
                 hidden, _, delta, _ = B.moe_post_attention(s, o_proj, attn, hidden, w.o_table, w.norm_moe, self.eps, w.Wr, w.page_table, w.page_pool, bias=w.bias)
             else:
                 hidden, _, delta, _ = B.moe_post_attention_i8(s, o_proj, attn, hidden, w.o_table, w.scales.o, w.norm_moe, self.eps, w.Wr, w.page_table, w.page_pool,
-                                                              w.scales.experts, bias=w.bias)
+                                                              w.scales.experts, bias=w.bias, workspace=space[256 * i:256 * i + need])
         out = hidden + delta
+        if space is not None and T:                  # without rows nothing was written there
+            self.status[:1] |= space.view(torch.int32)[:64 * len(self.layers):64].amax()          # bit 0 is the only one that a layer sets
         self.lengths, self.free_head, self._turn = tables.seq_len, tables.free_head, self._turn ^ 1
         return out, tables
 

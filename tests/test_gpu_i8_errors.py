@@ -1,9 +1,12 @@
 """Bad entries of page tables in the layer in 8-bit integers: read as page 0, and reported to whoever makes the call."""
+import dataclasses
+
 import pytest
 import torch
 
 import paper_2411_11217_amd as M
 from test_gpu_i8 import Linear, layer_inputs
+from test_gpu_i8_decode_layers import build
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +82,35 @@ def test_reports_of_a_captured_call():
             assert torch.equal(out[0], mid) and torch.equal(out[1], y)
         call(o_table, table)                     # eager work between the replays
         torch.cuda.synchronize()
+
+
+def steps(model, fresh, seed):
+    x = torch.randn((sum(fresh), 256), generator=torch.Generator().manual_seed(seed)).cuda()
+    return model.step(x, torch.tensor(fresh, dtype=torch.int32).cuda())[0]
+
+
+@pytest.mark.parametrize("field", ["o_table", "page_table", "qkv_table"])
+@pytest.mark.parametrize("layer", [0, 1, 2])
+def test_decode_layers_reports_its_weights(layer, field):
+    """A bad entry of any table of any layer sets bit 0 of the model's status, which stays until the caller clears it."""
+    layers, _, model = build(n_layers=3)
+    want = [steps(model, f, n) for n, f in enumerate(([5, 0, 2], [1, 1, 1], [1, 40, 1], [1, 1, 1]))]
+    assert model.status.tolist() == [0] * 4
+    _, _, model = build(n_layers=3)
+    good = getattr(layers[layer], field)
+    bad = good.clone()
+    bad.view(-1)[0] = -1                         # for the experts: of expert 0
+    if field == "page_table":
+        bad[:, 0] = -1
+    assert torch.equal(steps(model, [5, 0, 2], 0), want[0]) and model.status.tolist() == [0] * 4
+    model.layers[layer] = dataclasses.replace(model.layers[layer], **{field: bad})
+    steps(model, [1, 1, 1], 1)
+    assert model.status.tolist() == [1, 0, 0, 0]
+    model.layers[layer] = dataclasses.replace(model.layers[layer], **{field: good})
+    steps(model, [1, 40, 1], 2)
+    steps(model, [0, 0, 0], 2)
+    assert model.status.tolist() == [1, 0, 0, 0]
+    model.status.zero_()
+    steps(model, [1, 1, 1], 3)
+    assert model.status.tolist() == [0] * 4
+
