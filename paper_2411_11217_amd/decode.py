@@ -96,15 +96,17 @@ class DecodeLayers:
         space = None
         if s.dtype == B.DTYPE_I8:
             # One buffer for the layers' workspaces, each of which begins 256 bytes behind the one before: a layer writes over what is behind the beginnings of
-            # those before it, whose status words so stay until the end of the step, where they are looked at all at once.
+            # those before it, whose status words so stay until the end of the step, where they are looked at all at once.  Before them four words for the QKV
+            # projections, which beside the errors leave a reading of the clock in their status.
             need = B.post_attention_i8_workspace_bytes(s, o_proj)
-            space = B._scratch(need + 256 * len(self.layers), embedded.device)
+            space = B._scratch(need + 256 * (len(self.layers) + 1), embedded.device)
+            projections = space[:16].view(torch.int32).zero_()
         hidden, delta = None, embedded
-        for i, (w, (k_cache, v_cache)) in enumerate(zip(self.layers, self.caches)):
+        for i, (w, (k_cache, v_cache)) in enumerate(zip(self.layers, self.caches), 1):
             if w.scales is None:
                 hidden, _, qkv, _ = B.moe_pre_attention(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, want_bf16=False)
             else:
-                hidden, _, _, qkv = B.moe_pre_attention_i8(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, w.scales.qkv, status=self.status)
+                hidden, _, _, qkv = B.moe_pre_attention_i8(qkv_proj, hidden, delta, w.norm_attn, self.eps, w.qkv_table, w.page_pool, w.scales.qkv, status=projections)
             q = B.moe_qk_norm_rope(kv, qkv, self.inv_freq, tables.positions, tables.slots, k_cache, v_cache, w.q_gamma, w.k_gamma, self.eps, status=self.status)
             attn, _ = B.moe_attn_decode(kv, q, seen, self.block_table, k_cache, v_cache, window=self.window, table_row=tables.request,
                                         workspace=self._workspace, status=self.status)
@@ -115,8 +117,8 @@ class DecodeLayers:
                 hidden, _, delta, _ = B.moe_post_attention_i8(s, o_proj, attn, hidden, w.o_table, w.scales.o, w.norm_moe, self.eps, w.Wr, w.page_table, w.page_pool,
                                                               w.scales.experts, bias=w.bias, workspace=space[256 * i:256 * i + need])
         out = hidden + delta
-        if space is not None and T:                  # without rows nothing was written there
-            self.status[:1] |= space.view(torch.int32)[:64 * len(self.layers):64].amax()          # bit 0 is the only one that a layer sets
+        if space is not None and T:                  # without rows no layer has written there
+            self.status[:1] |= space.view(torch.int32)[:64 * (len(self.layers) + 1):64].amax()          # bit 0 is the only one that a layer sets
         self.lengths, self.free_head, self._turn = tables.seq_len, tables.free_head, self._turn ^ 1
         return out, tables
 

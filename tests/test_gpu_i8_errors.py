@@ -114,3 +114,14 @@ def test_decode_layers_reports_its_weights(layer, field):
     steps(model, [1, 1, 1], 3)
     assert model.status.tolist() == [0] * 4
 
+
+def test_decode_layers_status_holds_no_clock():
+    """A QKV launch of more than 256 blocks reports the clock that it saw: not as a status of the model, whose words 1 to 3 stay zero."""
+    layers, _, model = build(n_layers=1)
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    T = 20000
+    rows, scale = torch.ones((T, 256), dtype=torch.int8, device="cuda"), torch.ones(T, device="cuda")
+    M.moe_linear_i8(M.make_linear_shape(T, 256, 512, 65536, "i8"), rows, scale, layers[0].qkv_table, layers[0].page_pool, layers[0].scales.qkv, status=status)
+    assert status[0] == 0 and status[3] > 100    # so a step of this size has it too
+    model.step(torch.randn((T, 256), device="cuda"), torch.tensor([1, 1, 1], dtype=torch.int32).cuda())      # rows behind the third belong to no request
+    assert model.status.tolist() == [0] * 4
