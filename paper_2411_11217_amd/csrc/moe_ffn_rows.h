@@ -364,16 +364,19 @@ int down_rows(GemmParams& p, int H, int R, int rows_each, int n_exp, hipStream_t
 // 59 | 58 / 60 (with the blocks before).
 // Groups of wavefronts that split k change the order of the sums, which the O projection hands on to a rounding and the router: left out.  So are
 // two k-steps behind one barrier: within 5 % either way, the barriers are not what the launch waits for.
-// KG teams, of eight wavefronts two: sixteen wavefronts are the most, with 128 registers each.
+// KG teams, of eight wavefronts two: sixteen wavefronts are the most, with 128 registers each.  With teams the blocks of 32 rows, and of 64 rows and one group, are
+// launch_linear_i8's own, in other forms: by its rules no call comes here for them.
 template <class Op, int KG>
 int linear_rows(GemmParams& p, int N, int T, hipStream_t st) {
     static_assert(KG == 1 || KG == 4, "");
     const LinearBlock b = linear_rows_block(T, p.KT * kTileK, N);        // k as bf16 would have it in these bytes
     constexpr int K8 = KG < 2 ? KG : 2;
     if (b.rows == 128) return launch_rows<Op, 1, 8, 4, 1, 2, 4, K8>(p, N, T, 1, st);
-    if (b.rows == 32) return b.groups == 1 ? launch_rows<Op, 1, 2, 1, 1, 2, 8, KG>(p, N, T, 1, st) : launch_rows<Op, 1, 2, 2, 1, 2, KG == 4 ? 4 : 8, KG>(p, N, T, 1, st);
+    if constexpr (KG == 1) {
+        if (b.rows == 32) return b.groups == 1 ? launch_rows<Op, 1, 2, 1, 1, 2, 8>(p, N, T, 1, st) : launch_rows<Op, 1, 2, 2, 1, 2, 8>(p, N, T, 1, st);
+        if (b.groups == 1) return launch_rows<Op, 1, 4, 1, 1, 4, 8>(p, N, T, 1, st);
+    }
     switch (b.groups) {
-        case 1: return launch_rows<Op, 1, 4, 1, 1, 4, KG == 4 ? 4 : 8, KG>(p, N, T, 1, st);
         case 2: return launch_rows<Op, 1, 4, 2, 1, 2, KG == 4 ? 4 : 6, KG>(p, N, T, 1, st);
         case 4: return launch_rows<Op, 1, 4, 4, 1, 1, 4, KG>(p, N, T, 1, st);
         case 5: return launch_rows<Op, 1, 4, 5, 1, 1, 4, K8>(p, N, T, 1, st);

@@ -181,3 +181,101 @@ def assert_status_clean(status):
     st = [int(v) for v in status]
     assert st[0] == 0 and st[1] == 0, st
     return st
+
+
+def _i8_linear_block(T, K, N):
+    """linear_rows_block (csrc/moe_host.h)."""
+    groups, row_tiles = N // 16, (T + 63) // 64
+
+    def one_round(g):
+        return row_tiles * -(-groups // g) <= 256
+
+    def crowded(g):
+        return K >= 1536 and groups <= 8 * g and row_tiles * -(-groups // g) > 216
+
+    rows = 32 if T <= 32 else 64
+    for g in (1, 2):
+        if one_round(g) and not crowded(g):
+            return rows, g
+    if T <= 64 or one_round(4):
+        return 64, 4
+    tall = (N // 64) * ((T + 127) // 128) <= 256
+    if tall and T <= 96 and K <= 512:
+        return 128, 4
+    for g in (5, 6):
+        if one_round(g):
+            return 64, g
+    if tall and row_tiles % 2 and row_tiles < 32 and (T - 1) % 64 >= 24 and K >= (2 if row_tiles < 10 else 3) << 10:
+        return 128, 4
+    return 64, 8
+
+
+def i8_linear_launch(T, K, N):
+    """The kernel of launch_linear_i8 (csrc/moe_ffn_i8.hip), by its own formulas and with the options as they are: its name and template arguments behind the operands' kind."""
+    half_k, kt = K // 2, K // 128
+    if (N // 64) * ((T + 127) // 128) <= 256 or (half_k <= 1536 and T <= 32) or (T > 128 and ((T + 63) // 64) * (N // 128) <= 256):
+        tiles = (T + 31) // 32
+        if kt >= 20 and tiles * (N // 16) <= 256:
+            return "ffn_rows", 1, 2, 1, 1, 2, 4, 8
+        if kt >= 12 and tiles * (N // 32) <= 256:
+            return "ffn_rows", 1, 2, 2, 1, 2, 4, 4
+        if kt >= 20 and tiles * ((N // 16 + 2) // 3) <= 256:
+            return "ffn_rows", 1, 2, 3, 1, 1, 4, 4
+        teams = 1 if kt < 16 else 4
+        two = min(teams, 2)
+        rows, groups = _i8_linear_block(T, half_k, N)
+        if rows == 128:
+            return "ffn_rows", 1, 8, 4, 1, 2, 4, two
+        if rows == 32:
+            assert teams == 1                    # the three rules before take the others
+            return "ffn_rows", 1, 2, groups, 1, 2, 8, 1
+        if groups <= 4:
+            assert teams == 1 or groups > 1
+            return ("ffn_rows", 1, 4, groups) + {1: (1, 4, 8), 2: (1, 2, 4 if teams == 4 else 6), 4: (1, 1, 4)}[groups] + (teams,)
+        return "ffn_rows", 1, 4, groups, 1, 1, 4, two
+    tiles = N // 128
+    if (T // 256 + 1) * ((tiles + 1) // 2) >= 512:
+        return "ffn_gemm", 1, 2, 256, 0
+    half = ((T + 127) // 128) * tiles
+    return "ffn_gemm", 1, 1, 128 if T > 128 and half <= 256 and (T > 160 or half <= 224 or kt <= 32) else 256, 0
+
+
+def i8_expert_launches(T, H, F, E, k):
+    """(gate/up, down, p.stream) of launch_expert_ffn_i8, as i8_linear_launch says a kernel."""
+    each, dt = T * k // E, H // 128
+    none = (1.0 - k / E) ** T
+    neither = ((E - k) * (E - k - 1.0) / (E * (E - 1.0))) ** T if E > 1 else none
+    deviation = max(0.0, E * none * (1.0 - none) + E * (E - 1.0) * (neither - none * none)) ** 0.5
+    experts = E * (1.0 - none)
+    streams = each <= 256 and E * 3 * H * F > 128 << 20
+    stream = 0 if not streams else 2 if F >= 6144 and E * dt >= 256 else 1
+    if each <= 96:
+        tall = each > 44
+        if T <= 16 and experts * (F // 64) <= 440:
+            gate = "ffn_thin", 0, 2
+        else:
+            groups = F // 16
+
+            def longest(cw):
+                return -(-E * -(-groups // cw) // 256) * (2 * cw + 1)
+
+            wide = 4 if E * (groups // 8) < (64 if tall else 128) else 7 if tall and longest(7) < longest(8) else 8
+            gate = ("ffn_rows", 0) + ((8, wide, 1, 1, 2, 1) if tall else (4, wide, 1, 1, 4, 1))
+        blocks, kb = experts * dt, F // 2
+        if kb <= 2048:
+            thin = blocks < 190 or 256 < blocks < 500
+        else:
+            long_k = kb > 10240
+            thin = blocks < (190 if long_k else 130) or (blocks - (0.0 if long_k else 0.5 * deviation * dt) > 256 and min(blocks + deviation * dt, E * dt) <= 384)
+        if T <= 16 and thin:
+            down = "ffn_thin", 1, 1
+        elif tall:
+            down = "ffn_rows", 1, 8, 4 if 2 * E * dt <= 256 and F // 128 >= 12 else 8, 1, 1, 4, 1
+        else:
+            down = "ffn_rows", 1, 4, 2 if 4 * E * dt <= 256 else 4 if 2 * E * dt <= 256 else 8, 1, 1, 4, 1
+        return gate, down, stream
+    tiles = E * max(1, (each - 32 + 255) // 256)
+    gate = "ffn_gemm", 0, 2, 256, int(0 < tiles * (F // 128) % 256 <= 128)
+    if tiles * dt <= 256:
+        return gate, ("ffn_gemm", 1, 1, 256, int(tiles * dt <= 128)), stream
+    return gate, ("ffn_gemm", 1, 2, 256, 1), stream
