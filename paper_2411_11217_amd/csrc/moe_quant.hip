@@ -96,7 +96,8 @@ struct Piece<uint16_t, 8> {
 
 constexpr int kMostBlocks = 1 << 20;             // rows beyond theirs are taken in turn
 
-// live: device, or null: rows from *live on are left as they were.  clear: four words set to zero, or null.  WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is read twice.
+// live: device, or null: rows from *live on are left as they were.  clear: four words set to zero, or null.  WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is
+// read twice, without hints.
 template <class In, int VEC, int WAVES, int PER, bool FAR, bool PAST>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel(const In* __restrict__ x, int64_t row_elements, int T, int pieces, int8_t* __restrict__ q,
                                                                                  float* __restrict__ scale, const int32_t* __restrict__ live, int32_t* __restrict__ clear) {
@@ -151,9 +152,13 @@ template <class In, int VEC, int WAVES, int PER>
 int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, int32_t* clear, hipStream_t st) {
     const dim3 grid(std::min(WAVES == 1 ? T / 4 + (T % 4 != 0) : T, kMostBlocks)), block(WAVES == 1 ? 256 : 64 * WAVES);
     const bool far = (int64_t)T * pieces * VEC * ((int)sizeof(In) + 1) > kQuantizeFar;
-    if (past) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, true>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
-    else if (far) hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, true, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
-    else hipLaunchKernelGGL((quantize_kernel<In, VEC, WAVES, PER, false, false>), grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
+    auto kernel = quantize_kernel<In, VEC, WAVES, PER, false, false>;
+    if constexpr (PER > 0) {
+        if (far) kernel = quantize_kernel<In, VEC, WAVES, PER, true, false>;
+        if constexpr (VEC == 8)                  // h, whose rows are multiples of 256 bf16
+            if (past) kernel = quantize_kernel<In, VEC, WAVES, PER, true, true>;
+    }
+    hipLaunchKernelGGL(kernel, grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }

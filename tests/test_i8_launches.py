@@ -10,21 +10,25 @@ from paper_2411_11217_amd import build
 from util import i8_expert_launches, i8_linear_launch
 
 
-def kernels():
-    """(operands' kind, name, template arguments) of the library's kernels on 8-bit integers, by its symbols."""
+def symbols():
+    """The library's kernels, by the symbols of their handles on the host."""
     nm = shutil.which("nm") or shutil.which("llvm-nm", path="/opt/rocm/llvm/bin")
     if nm is None:
         pytest.skip("no nm")
     if build.is_stale():
         build.build()
     out = subprocess.run([nm, build.LIB], capture_output=True, text=True, check=True).stdout
-    found = set()
-    for line in out.splitlines():
-        symbol = line.split()[-1]
-        m = re.search(r"GLOBAL__N_1\d+(ffn_rows|ffn_thin|ffn_gemm)INS_4Int8I(f|DF16b)EE((?:L[ib]\d+E)+)E", symbol)
-        if m and line.split()[-2] in "dD":
-            found.add((m[2], m[1]) + tuple(int(v) for v in re.findall(r"L[ib](\d+)E", m[3])))
-    return found
+    return [line.split()[-1] for line in out.splitlines() if line.split()[-2] in "dD"]
+
+
+def arguments(text):
+    return tuple(int(v) for v in re.findall(r"L[ib](\d+)E", text))
+
+
+def kernels():
+    """(operands' kind, name, template arguments) of those that multiply 8-bit integers."""
+    found = (re.search(r"GLOBAL__N_1\d+(ffn_rows|ffn_thin|ffn_gemm)INS_4Int8I(f|DF16b)EE((?:L[ib]\d+E)+)E", s) for s in symbols())
+    return {(m[2], m[1]) + arguments(m[3]) for m in found if m}
 
 
 def test_every_linear_and_expert_kernel_is_reached_and_there():
@@ -39,3 +43,14 @@ def test_every_linear_and_expert_kernel_is_reached_and_there():
     held = kernels()
     assert reached - held == set()
     assert held - reached == set()
+
+
+def test_every_kernel_of_rows_in_8_bits_is_another():
+    """Element type, elements of a load, wavefronts to a row, loads of a thread, hint on loads, hint on stores: rows that are read twice have no hint, and the one on
+    stores is for h, which is read eight bf16 at a time."""
+    found = (re.search(r"quantize_kernelI([ft])((?:L[ib]\d+E)+)E", s) for s in symbols())
+    held = {(m[1],) + arguments(m[2]) for m in found if m}
+    lengths = [(1, 1), (1, 2), (4, 2), (8, 2), (16, 2), (16, 4)]
+    want = {(t, vec, waves, per, far, 0) for t, vec in (("f", 4), ("t", 4), ("t", 8)) for waves, per in lengths for far in (0, 1)}
+    want |= {("t", 8, waves, per, 1, 1) for waves, per in lengths} | {("f", 4, 16, 0, 0, 0), ("t", 4, 16, 0, 0, 0), ("t", 8, 16, 0, 0, 0)}
+    assert held == want
