@@ -19,8 +19,6 @@ __global__ __launch_bounds__(256) void combine_kernel(const Four* __restrict__ o
                                                       const float* __restrict__ topk_w, int k, int R, int row_vec,
                                                       float4* __restrict__ y, const int32_t* __restrict__ found, int32_t* __restrict__ status) {
     const int t = blockIdx.x;
-    if constexpr (std::is_same<Four, uint2>::value)
-        if (found && t == 0 && threadIdx.x == 0 && found[0]) atomicOr(status, found[0]);
     __shared__ int32_t rows[MOE_MAX_EXPERTS];
     __shared__ float wts[MOE_MAX_EXPERTS];
     if (threadIdx.x < k) {
@@ -41,6 +39,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const Four* __restrict__ o
         }
         y[(size_t)t * row_vec + c] = acc;
     }
+    if constexpr (std::is_same<Four, uint2>::value)
+        if (t == 0 && threadIdx.x == 0 && found && found[0]) atomicOr(status, found[0]);
 }
 
 }  // namespace

@@ -91,7 +91,7 @@ int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st)
     int rc = !few ? (half_round() ? launch_gate_up_halves_i8(p, R, s.E, st) : launch_gate_up_i8(p, R, s.E, st))
              : thin_takes_gate_up(s) ? launch_thin<ToFloat, 0, 2>(p, s.F, R, s.E, st) : launch_gate_up_few(p, s, R, rows_each, st);
     if (rc != MOE_OK) return rc;
-    rc = launch_quantize_i8(R, s.F, a.h, MOE_DTYPE_BF16, s.F, a.h_q, a.h_scale, p.stream != 0, a.offsets + s.E, st);
+    rc = launch_quantize_i8(R, s.F, a.h, MOE_DTYPE_BF16, s.F, a.h_q, a.h_scale, p.stream != 0, const_cast<int32_t*>(a.offsets) + s.E, false, st);      // only read
     if (rc != MOE_OK) return rc;
     fill_down(p, s, g, f);
     p.A = (const char*)a.h_q;

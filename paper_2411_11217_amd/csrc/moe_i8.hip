@@ -205,7 +205,7 @@ int moe_post_attention_i8(const moe_shape* s, const moe_linear_shape* o_proj, co
     float *a_scale = (float*)(ws + L.a_scale), *x_scale = (float*)(ws + L.x_scale), *o = (float*)(ws + L.o);
     // The router clears the layer's status words behind the O projection, which therefore has its own: cleared with attn's rows, joined to the others by the combine.
     int32_t* const found = (int32_t*)(ws + L.found);
-    rc = launch_quantize_i8(s->T, o_proj->K, attn, MOE_DTYPE_BF16, o_proj->K, a_q, a_scale, false, nullptr, st, found);
+    rc = launch_quantize_i8(s->T, o_proj->K, attn, MOE_DTYPE_BF16, o_proj->K, a_q, a_scale, false, found, true, st);
     if (rc != MOE_OK) return rc;
     rc = enqueue_linear(*o_proj, a_q, a_scale, o_table, page_pool, pool_pages, o_scale, o, found, st);
     if (rc != MOE_OK) return rc;

@@ -117,8 +117,8 @@ struct FfnI8Args {
     int32_t* status;
 };
 int launch_expert_ffn_i8(const moe_shape& s, const FfnI8Args& a, hipStream_t st);
-int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live,
-                       hipStream_t st, int32_t* clear = nullptr);      // past: q past the L2; live: device, or null: rows from *live on are left as they were; clear: four words set to zero
+int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, int32_t* words,
+                       bool clear, hipStream_t st);          // past: q past the L2; words: device, or null: rows from *words on are left as they were, with `clear` four words set to zero
 bool norm_takes(int32_t H, float eps);
 int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* q, float* scale,
                           hipStream_t st);

@@ -96,18 +96,21 @@ struct Piece<uint16_t, 8> {
 
 constexpr int kMostBlocks = 1 << 20;             // rows beyond theirs are taken in turn
 
-// live: device, or null: rows from *live on are left as they were.  clear: four words set to zero, or null.  WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is
+// words: device, or null: rows from *words on are left as they were, or with `clear` four words that are set to zero.  WAVES wavefronts to a row; with one, four rows to a block.  PER pieces to a thread stay in registers as they came; with PER = 0 the row is
 // read twice, without hints.
 template <class In, int VEC, int WAVES, int PER, bool FAR, bool PAST>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel(const In* __restrict__ x, int64_t row_elements, int T, int pieces, int8_t* __restrict__ q,
-                                                                                 float* __restrict__ scale, const int32_t* __restrict__ live, int32_t* __restrict__ clear) {
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel(const In* __restrict__ x, int64_t row_elements, int T, int pieces, bool clear, int8_t* __restrict__ q,
+                                                                                 float* __restrict__ scale, int32_t* __restrict__ words) {
     typedef Piece<In, VEC> P;
     __shared__ uint32_t part[WAVES];
     constexpr int kRows = WAVES == 1 ? 4 : 1, kThreads = 64 * WAVES;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int me = WAVES == 1 ? lane : threadIdx.x;
-    const int rows = live ? min(T, *live) : T;   // wanted at the first store only
-    if (clear && blockIdx.x == 0 && threadIdx.x < 4) clear[threadIdx.x] = 0;
+    int rows = T;
+    if (words) {                                 // one argument for both: with another, every launch took 0.1 to 0.6 us more
+        if (!clear) rows = min(T, *words);       // wanted at the first store only
+        else if (blockIdx.x == 0 && threadIdx.x < 4) words[threadIdx.x] = 0;
+    }
     for (int64_t t = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0); t < T; t += (int64_t)gridDim.x * kRows) {
         const In* const row = x + t * row_elements;
         int8_t* const out = q + t * pieces * VEC;
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void quantize_kernel
 }
 
 template <class In, int VEC, int WAVES, int PER>
-int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, int32_t* clear, hipStream_t st) {
+int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, int32_t* words, bool clear, hipStream_t st) {
     const dim3 grid(std::min(WAVES == 1 ? T / 4 + (T % 4 != 0) : T, kMostBlocks)), block(WAVES == 1 ? 256 : 64 * WAVES);
     const bool far = (int64_t)T * pieces * VEC * ((int)sizeof(In) + 1) > kQuantizeFar;
     auto kernel = quantize_kernel<In, VEC, WAVES, PER, false, false>;
@@ -158,7 +161,7 @@ int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t
         if constexpr (VEC == 8)                  // h, whose rows are multiples of 256 bf16
             if (past) kernel = quantize_kernel<In, VEC, WAVES, PER, true, true>;
     }
-    hipLaunchKernelGGL(kernel, grid, block, 0, st, x, row_elements, T, pieces, q, scale, live, clear);
+    hipLaunchKernelGGL(kernel, grid, block, 0, st, x, row_elements, T, pieces, clear, q, scale, words);
     MOE_HIP_TRY(hipGetLastError());
     return MOE_OK;
 }
@@ -166,15 +169,15 @@ int launch_quantize(int T, int pieces, const In* x, int64_t row_elements, int8_t
 // Wavefronts by the length of the row alone: a row's loads are then under way at once, and what is in flight fills the chip.  us, 256 threads to
 // every row / these: 512 x 14336 9.1 / 5.9, 8192 x 14336 88 / 64, 60000 x 256 53 / 17, 1 x 28672 10.4 / 3.2.
 template <class In, int VEC>
-int launch_quantize(int T, int N, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, int32_t* clear, hipStream_t st) {
+int launch_quantize(int T, int N, const In* x, int64_t row_elements, int8_t* q, float* scale, bool past, int32_t* words, bool clear, hipStream_t st) {
     const int pieces = N / VEC;
-    if (pieces <= 64) return launch_quantize<In, VEC, 1, 1>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
-    if (pieces <= 128) return launch_quantize<In, VEC, 1, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
-    if (pieces <= 512) return launch_quantize<In, VEC, 4, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
-    if (pieces <= 1024) return launch_quantize<In, VEC, 8, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
-    if (pieces <= 2048) return launch_quantize<In, VEC, 16, 2>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
-    if (pieces <= 4096) return launch_quantize<In, VEC, 16, 4>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
-    return launch_quantize<In, VEC, 16, 0>(T, pieces, x, row_elements, q, scale, past, live, clear, st);
+    if (pieces <= 64) return launch_quantize<In, VEC, 1, 1>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
+    if (pieces <= 128) return launch_quantize<In, VEC, 1, 2>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
+    if (pieces <= 512) return launch_quantize<In, VEC, 4, 2>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
+    if (pieces <= 1024) return launch_quantize<In, VEC, 8, 2>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
+    if (pieces <= 2048) return launch_quantize<In, VEC, 16, 2>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
+    if (pieces <= 4096) return launch_quantize<In, VEC, 16, 4>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
+    return launch_quantize<In, VEC, 16, 0>(T, pieces, x, row_elements, q, scale, past, words, clear, st);
 }
 
 // Residual and norm: one pass over the rows.  s = hidden + delta stays in registers, its squares are added up, then the magnitudes of y are
@@ -272,10 +275,10 @@ int launch_norm(const NormArgs& a, hipStream_t st) {
 
 namespace moe {
 
-int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, const int32_t* live, hipStream_t st, int32_t* clear) {
-    if (x_dtype == MOE_DTYPE_F32) return launch_quantize<float, 4>(T, N, (const float*)x, row_elements, q, scale, past, live, clear, st);
-    if (N % 8 == 0 && row_elements % 8 == 0 && aligned16(x) && (uintptr_t)q % 8 == 0) return launch_quantize<uint16_t, 8>(T, N, (const uint16_t*)x, row_elements, q, scale, past, live, clear, st);
-    return launch_quantize<uint16_t, 4>(T, N, (const uint16_t*)x, row_elements, q, scale, past, live, clear, st);
+int launch_quantize_i8(int T, int N, const void* x, int x_dtype, int64_t row_elements, int8_t* q, float* scale, bool past, int32_t* words, bool clear, hipStream_t st) {
+    if (x_dtype == MOE_DTYPE_F32) return launch_quantize<float, 4>(T, N, (const float*)x, row_elements, q, scale, past, words, clear, st);
+    if (N % 8 == 0 && row_elements % 8 == 0 && aligned16(x) && (uintptr_t)q % 8 == 0) return launch_quantize<uint16_t, 8>(T, N, (const uint16_t*)x, row_elements, q, scale, past, words, clear, st);
+    return launch_quantize<uint16_t, 4>(T, N, (const uint16_t*)x, row_elements, q, scale, past, words, clear, st);
 }
 
 int launch_add_rmsnorm_i8(int T, int H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* q, float* scale,
@@ -302,7 +305,7 @@ int moe_quantize_i8(int32_t T, int32_t N, const void* x, int32_t x_dtype, int64_
     const int64_t esize = x_dtype == MOE_DTYPE_F32 ? 4 : 2, x_bytes = ((T - 1) * row_elements + N) * esize, q_bytes = (int64_t)T * N, s_bytes = (int64_t)T * 4;
     if (!x || !x_q || !x_scale || (uintptr_t)x % (4 * esize) != 0 || (uintptr_t)x_q % 4 != 0 || (uintptr_t)x_scale % 4 != 0) return MOE_ERR_INVALID_ARG;
     if (overlap(x, x_bytes, x_q, q_bytes) || overlap(x, x_bytes, x_scale, s_bytes) || overlap(x_q, q_bytes, x_scale, s_bytes)) return MOE_ERR_INVALID_ARG;
-    return launch_quantize_i8(T, N, x, x_dtype, row_elements, x_q, x_scale, false, nullptr, (hipStream_t)stream);
+    return launch_quantize_i8(T, N, x, x_dtype, row_elements, x_q, x_scale, false, nullptr, false, (hipStream_t)stream);
 }
 
 int moe_add_rmsnorm_i8(int32_t T, int32_t H, const float* hidden, const float* delta, const float* gamma, float eps, float* hidden_out, void* x_out, int8_t* x_q,

@@ -100,7 +100,8 @@ class DecodeLayers:
             # projections, which beside the errors leave a reading of the clock in their status.
             need = B.post_attention_i8_workspace_bytes(s, o_proj)
             space = B._scratch(need + 256 * (len(self.layers) + 1), embedded.device)
-            projections = space[:16].view(torch.int32).zero_()
+            words = space.view(torch.int32)
+            projections = words[:4].zero_()
         hidden, delta = None, embedded
         for i, (w, (k_cache, v_cache)) in enumerate(zip(self.layers, self.caches), 1):
             if w.scales is None:
@@ -118,7 +119,7 @@ class DecodeLayers:
                                                               w.scales.experts, bias=w.bias, workspace=space[256 * i:256 * i + need])
         out = hidden + delta
         if space is not None and T:                  # without rows no layer has written there
-            self.status[:1] |= space.view(torch.int32)[:64 * (len(self.layers) + 1):64].amax()          # bit 0 is the only one that a layer sets
+            self.status[:1].bitwise_or_(words[:64 * (len(self.layers) + 1):64].amax())          # bit 0 is the only one that a layer sets
         self.lengths, self.free_head, self._turn = tables.seq_len, tables.free_head, self._turn ^ 1
         return out, tables
 
