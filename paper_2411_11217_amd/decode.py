@@ -63,7 +63,8 @@ class DecodeLayers:
         self.inv_freq, self.eps, self.window = inv_freq, float(eps), int(window)
         width = (kv.n_q + 2 * kv.n_kv) * kv.head_dim
         self.qkv_width, self.attn_width = -(-width // 128) * 128, kv.n_q * kv.head_dim
-        for status in (B.kv_validate(kv), B.validate_shape(shape)):
+        norm = B._lib().moe_add_rmsnorm(0, shape.H, None, None, None, self.eps, None, None, None)          # no rows: the sizes alone
+        for status in (B.kv_validate(kv), B.validate_shape(shape), norm):
             B._check(status, "DecodeLayers")
         for K, N in ((shape.H, self.qkv_width), (self.attn_width, shape.H)):
             B.linear_pages_required(B.make_linear_shape(1, K, N, shape.page_bytes, shape.dtype))         # raises where the projections do not take such sizes
