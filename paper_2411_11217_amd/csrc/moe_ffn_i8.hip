@@ -34,6 +34,7 @@ constexpr int64_t kHintBytes = (int64_t)128 << 20;
 
 // Blocks of the kernel for few rows: 64 rows up to kRows64Max per expert on average, else 128.  Features per block: 128, which read the rows half as often as 64, where these are blocks enough.  us for the
 // call, 64 / 128: 2048 x 4096 160 tokens (256 blocks of 128) 53.6 / 52.4, 64 experts of 2048 x 1024 320 tokens 87.0 / 85.3, 1024 x 2816 64 tokens 31.4 / 30.3, 5 experts of 1280 x 768 (30) 26 tokens 18.1 / 20.3, 133: 23.8 / 24.8.
+// Where 64 take over, below 64 or 128 blocks, was looked at on the last of these alone, whose 30 are far below either.
 //   With more than kRows64Max rows 112 where a compute unit then has less to read: it has weights from HBM at 25 GB/s whatever the others do, so the one with the most blocks is what the launch waits for.  112 / 128:
 // Mixtral-8x7B shape 256 tokens (1024 blocks, four to a compute unit / 896, three and a half) 245.6 / 249.2, DBRX shape 320 tokens (six / five and a quarter) 551 / 558, but 2048 x 4096 256 tokens (296 / 256) 67.4 / 56.0.
 static int launch_gate_up_few(GemmParams& p, const moe_shape& s, int R, int rows_each, hipStream_t st) {
@@ -47,7 +48,7 @@ static int launch_gate_up_few(GemmParams& p, const moe_shape& s, int R, int rows
 
 // Columns per block: 128, or 64 or 32 where they still make one round and 128 leave compute units without a block.  us for the call, 128 / 64 / 32: 2048 x 4096 64 tokens (128 blocks of 128) 47.9 / 44.8 / 44.6, 256: 56.3 / 52.7 /
 // 57.6; 1024 x 2816 64 tokens (64) 31.3 / 28.7 / 28.1, 256: 36.6 / 34.9 / 34.4; 5 experts of 1280 x 768 66 tokens (50) 20.3 / 19.6 / 19.6, but 106 tokens (128 rows to a block, six k-steps) 24.2 / 24.9 / 25.2; Mixtral-8x7B shape 64 (256)
-// 230 / 231 / 233, 256: 250 / 263 / 293.
+// 230 / 231 / 233, 256: 250 / 263 / 293.  The twelve k-steps lie between the six of that shape and the 22 of 1024 x 2816; nothing between them was measured.
 static int launch_down_few(GemmParams& p, const moe_shape& s, int R, int rows_each, hipStream_t st) {
     const int64_t blocks = (int64_t)s.E * (s.H / 128);
     if (rows_each > kRows64Max) {
